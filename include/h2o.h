@@ -331,6 +331,118 @@ int h2o_kv_gather(const void* cache, const int32_t* idx, void* delta, int B,
 int h2o_kv_scatter(void* cache, const int32_t* idx, const void* src, int B,
                    int Hkv, int M, int k, int d, int dtype, void* stream);
 
+/* ---- The cache in 8 bits (Sec. "Fine-Tuning for Sparse Attention": the paper
+ * keeps its cache buffers quantised to 8 bits).
+ *
+ * A row x of d keys or values is held as d signed bytes (codes) and one float32
+ * scale:
+ *        k_codes, v_codes      [B, Hkv, M, d]       int8
+ *        k_scales, v_scales    [B, Hkv, M]          float32
+ *   scale = max|x| / 127 (rounded to float32), code = x / scale rounded to the
+ *   nearest integer, ties to even; the value that a code stands for is
+ *   code * scale, off x by at most scale / 2 (plus the scale's own rounding).
+ * A row whose scale would be below 2^-126 (the smallest normal float32) is held as
+ * zeros with scale 0. A row with an Inf or NaN has scale NaN and codes 0: it reads
+ * back as NaN, and a query that attends it gets NaN.
+ * dtype is that of the rows on the other side (q, k_new, v_new, out, ...). All
+ * limits of the shapes above hold; B * Hkv <= 65535 where there are queries, and
+ * B * Hkv * k < 2^28 rows. */
+
+/* k rows of K and of V per (b, KV head) into the cache: row i to slot idx[b,h,i]
+ * (idx [B,Hkv,k] int32; entries outside [0, M) are skipped, the others must be
+ * distinct within a head) or, with idx NULL, to slot i. k_src, v_src
+ * [B,Hkv,k,d] in dtype, 0 <= k <= M. Other slots are left as they are. */
+int h2o_kv_quantize(const void* k_src, const void* v_src, const int32_t* idx,
+                    int8_t* k_codes, float* k_scales, int8_t* v_codes,
+                    float* v_scales, int B, int Hkv, int M, int k, int d,
+                    int dtype, void* stream);
+
+/* The reverse: k_dst, v_dst [B,Hkv,k,d] = code * scale of slot idx[b,h,i] (or i),
+ * one float32 product, rounded to dtype; rows of entries outside [0, M) are left
+ * as they are. Training reads the cache back and takes h2o_sdpa_chunk and
+ * its backward: gradients pass the rounding straight through. */
+int h2o_kv_dequantize(const int8_t* k_codes, const float* k_scales,
+                      const int8_t* v_codes, const float* v_scales,
+                      const int32_t* idx, void* k_dst, void* v_dst, int B, int Hkv,
+                      int M, int k, int d, int dtype, void* stream);
+
+/* Bytes of device scratch for h2o_sdpa_chunk_q8 (policy H2O_POLICY_H2O) or for
+ * h2o_chunk_step_q8 with `policy` (0 on invalid arguments). */
+size_t h2o_q8_workspace_bytes(int B, int Hq, int Hkv, int T, int M, int d,
+                              int dtype, int policy);
+
+/* h2o_sdpa_chunk over an 8-bit cache: the results are those of the attention over
+ * the values that the codes stand for, without rounding these to dtype (the
+ * scales enter the scores and the probabilities in float32). The chunk's own
+ * keys and values are in dtype. M may be 0 (the cache pointers may be NULL then). */
+int h2o_sdpa_chunk_q8(const void* q, const int8_t* k_codes, const float* k_scales,
+                      const int8_t* v_codes, const float* v_scales,
+                      const void* k_new, const void* v_new, void* out, float* lse,
+                      float* wsum, void* workspace, size_t workspace_bytes, int B,
+                      int Hq, int Hkv, int T, int M, int d, float scale, int dtype,
+                      void* stream);
+
+/* h2o_evict_insert_policy over an 8-bit cache: the chunk's rows go into the
+ * evicted slots as h2o_kv_quantize writes them. */
+int h2o_evict_insert_q8(int8_t* k_codes, float* k_scales, int8_t* v_codes,
+                        float* v_scales, float* scores, int32_t* token_pos,
+                        const void* k_new, const void* v_new, const float* wsum,
+                        int32_t* evict_idx, int B, int Hkv, int M, int T, int d,
+                        int k, int32_t pos0, int dtype, int policy, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/* h2o_sdpa_chunk_q8, h2o_accumulate_scores and h2o_evict_insert_q8 (k = T) in one
+ * call, with the results of the three; M >= T. token_pos may be NULL except for
+ * H2O_POLICY_NORM. For T == 1 in bf16 with H2O_POLICY_H2O the attention, the
+ * ranking and the insert are two or three kernel launches. */
+int h2o_chunk_step_q8(const void* q, int8_t* k_codes, float* k_scales,
+                      int8_t* v_codes, float* v_scales, float* scores,
+                      int32_t* token_pos, const void* k_new, const void* v_new,
+                      void* out, float* lse, float* wsum, int32_t* evict_idx,
+                      void* workspace, size_t workspace_bytes, int B, int Hq, int Hkv,
+                      int T, int M, int d, float scale, int32_t pos0, int dtype,
+                      int policy, void* stream);
+
+/* ---- A tree of drafted tokens over the cache (speculative decoding). The T new
+ * tokens are nodes: parents [B,T] int32 holds for node i its parent's index, in
+ * [0, i), or -1 where it follows the last token before the draft (other values
+ * count as -1). A node sees every cache slot, its ancestors and itself; a chain
+ * (parents i - 1) is the causal chunk.
+ *
+ * The cache is in dtype (k_scales and v_scales NULL) or in 8 bits (k_cache and
+ * v_cache are int8 codes, both scales given). */
+
+/* Bytes of device scratch for h2o_sdpa_tree and for h2o_tree_accept with any path
+ * of a tree of T nodes (0 on invalid arguments). */
+size_t h2o_tree_workspace_bytes(int B, int Hq, int Hkv, int T, int M, int d,
+                                int dtype);
+
+/* out [B,Hq,T,d] and lse [B,Hq,T] of the T nodes, as in h2o_sdpa_chunk. The cache
+ * and the scores are left as they are: which of the nodes become tokens is not
+ * known yet. */
+int h2o_sdpa_tree(const void* q, const void* k_cache, const float* k_scales,
+                  const void* v_cache, const float* v_scales, const void* k_new,
+                  const void* v_new, const int32_t* parents, void* out, float* lse,
+                  void* workspace, size_t workspace_bytes, int B, int Hq, int Hkv,
+                  int T, int M, int d, float scale, int dtype, void* stream);
+
+/* What the eviction needs of the accepted nodes: path [B,A] int32 holds A nodes of
+ * the tree from a root on, each the parent of the next, 1 <= A <= T (the same A
+ * for every b; entries outside [0, T) stand for no token). With lse from
+ * h2o_sdpa_tree and the same q, cache, k_new and v_new:
+ *   wsum[b,h,j]     = sum_{hq in group h} sum_a exp(s_{path a, j} - lse_{path a})
+ *   wsum[b,h,M + c] = the same over the nodes a >= c, for the key of node path c
+ *   k_acc[b,h,a,:]  = k_new[b,h,path a,:], v_acc likewise  ([B,Hkv,A,d], dtype)
+ * (columns, rows and weights of entries that stand for no token are 0): wsum,
+ * k_acc and v_acc are then the chunk of A tokens for h2o_accumulate_scores and
+ * h2o_evict_insert, h2o_evict_insert_policy or h2o_evict_insert_q8. v_scales has
+ * no part in it. */
+int h2o_tree_accept(const void* q, const void* k_cache, const float* k_scales,
+                    const void* k_new, const void* v_new, const float* lse,
+                    const int32_t* path, void* k_acc, void* v_acc, float* wsum,
+                    void* workspace, size_t workspace_bytes, int B, int Hq, int Hkv,
+                    int T, int M, int A, int d, float scale, int dtype, void* stream);
+
 /* The selection of h2o_evict_insert alone: for each of `rows` rows of M
  * float32 scores, the k smallest by (score, index), ascending indices, into
  * idx_out [rows, k]. 0 <= k <= M. */
@@ -368,7 +480,10 @@ int h2o_debug_force_path(int path);
  *  18 backward dQ split reduce (MFMA path)
  *  19 bottom-k and insert in one launch (1 < k <= 4096)
  *  20 float32 attention (matrix cores)
- *  21 decode argmin and insert (h2o_chunk_step, T == 1, long caches) */
+ *  21 decode argmin and insert (h2o_chunk_step, T == 1, long caches)
+ *  22 8-bit rows, written or read back   23 one-sweep attention
+ *  24 its key ranges merged   25 column sums   26 their row ranges added
+ *  27 ancestor bits of a tree */
 int h2o_debug_timing(int on);
 int h2o_debug_kernel_time(int kernel_id, double* total_ms, long* count);
 

@@ -6,6 +6,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <string>
 #include <vector>
@@ -908,6 +909,330 @@ int h2o_kv_gather(const void* cache, const int32_t* idx, void* delta, int B, int
 int h2o_kv_scatter(void* cache, const int32_t* idx, const void* src, int B, int Hkv, int M, int k,
                    int d, int dtype, void* stream) {
   return kv_copy_call(false, cache, idx, const_cast<void*>(src), B, Hkv, M, k, d, dtype, stream);
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------- 8-bit cache and tree
+namespace h2o {
+namespace {
+
+bool all_aligned(std::initializer_list<const void*> ptrs) {
+  for (const void* p : ptrs)
+    if (!aligned16(p)) return false;
+  return true;
+}
+
+// Shape limits of the kernels behind the 8-bit cache and the tree: those of
+// check_shape, and one grid row per KV head.
+int check_flash_shape(int B, int Hq, int Hkv, int T, int M, int d) {
+  const int rc = check_shape(B, Hq, Hkv, T, M, d);
+  if (rc) return rc;
+  if ((long long)B * Hkv > 65535) return fail(H2O_ESHAPE, "B * Hkv must be <= 65535");
+  return H2O_OK;
+}
+
+int check_scale(float scale) {
+  if (!(std::isfinite(scale) && scale > 0.f)) return fail(H2O_EINVAL, "scale must be finite > 0");
+  return H2O_OK;
+}
+
+int launched(hipError_t e) {
+  if (e != hipSuccess) return fail(H2O_ELAUNCH, "kernel launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+// k rows per head into or out of an 8-bit cache of M slots.
+int check_rows_q8(int B, int Hkv, int M, int k, int d, int dtype) {
+  if (dtype != H2O_F32 && dtype != H2O_BF16) return fail(H2O_EDTYPE, "dtype %d unknown", dtype);
+  if (B < 1 || Hkv < 1 || M < 1 || k < 0 || k > M)
+    return fail(H2O_ESHAPE, "need B, Hkv, M >= 1 and 0 <= k <= M");
+  if (d != 64 && d != 128) return fail(H2O_ESHAPE, "head dim d=%d not supported (64 or 128)", d);
+  if ((long long)B * Hkv >= (1 << 24) || (long long)B * Hkv * k >= (1 << 28) ||
+      (long long)B * Hkv * M * d >= (1ll << 40))
+    return fail(H2O_ESHAPE, "too large");
+  return H2O_OK;
+}
+
+int kv_quant_call(bool write, void* k_rows, void* v_rows, const int32_t* idx, const CacheQ8& c,
+                  int B, int Hkv, int M, int k, int d, int dtype, void* stream) {
+  int rc = check_rows_q8(B, Hkv, M, k, d, dtype);
+  if (rc) return rc;
+  if (k > 0 && (!k_rows || !v_rows || !c.k || !c.ks || !c.v || !c.vs))
+    return fail(H2O_EINVAL, "null tensor pointer");
+  if (!all_aligned({k_rows, v_rows, idx, c.k, c.ks, c.v, c.vs}))
+    return fail(H2O_EALIGN, "tensor pointer not 16-byte aligned");
+  rc = check_device();
+  if (rc) return rc;
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  const bool f32 = dtype == H2O_F32;
+  return launched(write ? launch_kv_quantize(k_rows, v_rows, idx, c, B * Hkv, M, k, d, f32, st)
+                        : launch_kv_dequantize(c, idx, k_rows, v_rows, B * Hkv, M, k, d, f32, st));
+}
+
+// One token per query head in bf16 takes the token kernels.
+bool token_q8(int Hq, int Hkv, int T, int d, int dtype) {
+  return dtype == H2O_BF16 && T == 1 && decode_supports(d, Hq / Hkv);
+}
+size_t attend_q8_bytes(int B, int Hq, int Hkv, int T, int M, int d, int dtype) {
+  return align256(token_q8(Hq, Hkv, T, d, dtype)
+                      ? path_plan(Shape{B, Hq, Hkv, T, M, d}, 2).bytes
+                      : flash_plan(FlashShape{B, Hq, Hkv, T, M, d, dtype == H2O_F32}, false).bytes);
+}
+
+// Validation shared by the calls that attend over an 8-bit cache; ews: bytes of
+// the policy's own scratch behind the attention's.
+int check_attend_q8(const void* q, const CacheQ8& c, const void* k_new, const void* v_new,
+                    const void* out, const float* lse, const float* wsum, const void* workspace,
+                    size_t workspace_bytes, int B, int Hq, int Hkv, int T, int M, int d,
+                    float scale, int dtype, size_t ews) {
+  if (dtype != H2O_F32 && dtype != H2O_BF16) return fail(H2O_EDTYPE, "dtype %d unknown", dtype);
+  int rc = check_flash_shape(B, Hq, Hkv, T, M, d);
+  if (!rc) rc = check_scale(scale);
+  if (rc) return rc;
+  if (!q || !k_new || !v_new || !out || !lse || !wsum ||
+      (M > 0 && (!c.k || !c.ks || !c.v || !c.vs)))
+    return fail(H2O_EINVAL, "null tensor pointer");
+  if (!all_aligned({q, c.k, c.ks, c.v, c.vs, k_new, v_new, out, lse, wsum, workspace}))
+    return fail(H2O_EALIGN, "tensor pointer not 16-byte aligned");
+  const size_t need = attend_q8_bytes(B, Hq, Hkv, T, M, d, dtype) + ews;
+  if (workspace_bytes < need || (need > 0 && !workspace))
+    return fail(H2O_EWORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, need);
+  return H2O_OK;
+}
+
+hipError_t launch_attend_q8(const void* q, const CacheQ8& c, const void* k_new, const void* v_new,
+                            void* out, float* lse, float* wsum, char* ws, int B, int Hq, int Hkv,
+                            int T, int M, int d, float scale, int dtype, hipStream_t st) {
+  if (token_q8(Hq, Hkv, T, d, dtype)) {
+    const Shape s{B, Hq, Hkv, T, M, d};
+    return launch_sdpa_decode_q8(s, path_plan(s, 2), q, c, k_new, v_new, out, lse, wsum, ws, scale,
+                                 st);
+  }
+  const FlashShape s{B, Hq, Hkv, T, M, d, dtype == H2O_F32};
+  const FlashPlan p = flash_plan(s, false);
+  const FlashIn in{true, q, c.k, c.v, c.ks, c.vs, k_new, v_new};
+  hipError_t e = (s.f32 ? launch_flash_f32 : launch_flash)(s, p, in, false, out, lse, ws, scale, st);
+  if (e != hipSuccess) return e;
+  return (s.f32 ? launch_columns_f32 : launch_columns)(s, p, in, lse, nullptr, 0, nullptr, nullptr,
+                                                       wsum, ws, scale, st);
+}
+
+// The ranking of `policy` against age t, then the chunk's rows in 8 bits, scores
+// and positions into the k slots. ews: scratch of evict_workspace().
+hipError_t launch_evict_q8(int policy, const CacheQ8& c, float* scores, int32_t* token_pos,
+                           const void* k_new, const void* v_new, const float* wsum,
+                           int32_t* evict_idx, int B, int Hkv, int M, int T, int d, int k,
+                           int32_t pos0, int32_t t, bool f32, char* ews, hipStream_t st) {
+  const int rows = B * Hkv;
+  float* keys = reinterpret_cast<float*>(ews);
+  hipError_t e = hipSuccess;
+  if (policy == H2O_POLICY_ORIG) {
+    int32_t* head_idx = reinterpret_cast<int32_t*>(ews + align256((size_t)Hkv * M * 4));
+    e = launch_orig_keys(scores, keys, B, Hkv, M, st);
+    if (e == hipSuccess) e = launch_bottomk(keys, Hkv, M, k, head_idx, st);
+    if (e == hipSuccess) e = launch_broadcast_rows(head_idx, evict_idx, B, Hkv * k, st);
+  } else if (policy == H2O_POLICY_NORM) {
+    e = launch_norm_keys(scores, token_pos, keys, rows, M, t, st);
+    if (e == hipSuccess) e = launch_bottomk(keys, rows, M, k, evict_idx, st);
+  } else {
+    e = launch_bottomk(scores, rows, M, k, evict_idx, st);
+  }
+  if (e != hipSuccess) return e;
+  return launch_kv_quantize(k_new, v_new, evict_idx, c, rows, M, k, d, f32, st, scores, token_pos,
+                            wsum, T, pos0);
+}
+
+int check_evict_q8(const CacheQ8& c, const float* scores, const int32_t* token_pos,
+                   const void* k_new, const void* v_new, const float* wsum,
+                   const int32_t* evict_idx, int B, int Hkv, int M, int T, int d, int k, int dtype,
+                   int policy) {
+  if (T < 1) return fail(H2O_EINVAL, "chunk length T must be >= 1");
+  if (k != T) return fail(H2O_EINVAL, "k (%d) must equal T (%d): every chunk key is inserted", k, T);
+  if (M < k) return fail(H2O_EINVAL, "cache length M (%d) must be >= k (%d)", M, k);
+  int rc = check_rows_q8(B, Hkv, M, k, d, dtype);
+  if (!rc) rc = check_policy(policy, token_pos);
+  if (rc) return rc;
+  if (!c.k || !c.ks || !c.v || !c.vs || !scores || !k_new || !v_new || !wsum || !evict_idx)
+    return fail(H2O_EINVAL, "null tensor pointer");
+  if (!all_aligned({c.k, c.ks, c.v, c.vs, scores, token_pos, k_new, v_new, wsum, evict_idx}))
+    return fail(H2O_EALIGN, "tensor pointer not 16-byte aligned");
+  return H2O_OK;
+}
+
+// Validation shared by the tree's two calls. The scales' presence says whether
+// the cache is in 8 bits.
+int check_tree(const void* q, const void* k_cache, const float* k_scales, const void* k_new,
+               const void* v_new, const void* ints, const void* workspace, size_t workspace_bytes,
+               int B, int Hq, int Hkv, int T, int M, int d, float scale, int dtype) {
+  if (dtype != H2O_F32 && dtype != H2O_BF16) return fail(H2O_EDTYPE, "dtype %d unknown", dtype);
+  int rc = check_flash_shape(B, Hq, Hkv, T, M, d);
+  if (!rc) rc = check_scale(scale);
+  if (rc) return rc;
+  if (!q || !k_new || !v_new || !ints || (M > 0 && !k_cache))
+    return fail(H2O_EINVAL, "null tensor pointer");
+  if (!all_aligned({q, k_cache, k_scales, k_new, v_new, ints, workspace}))
+    return fail(H2O_EALIGN, "tensor pointer not 16-byte aligned");
+  const size_t need =
+      align256(flash_plan(FlashShape{B, Hq, Hkv, T, M, d, dtype == H2O_F32}, true).bytes);
+  if (workspace_bytes < need || (need > 0 && !workspace))
+    return fail(H2O_EWORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, need);
+  return H2O_OK;
+}
+
+}  // namespace
+}  // namespace h2o
+
+extern "C" {
+
+int h2o_kv_quantize(const void* k_src, const void* v_src, const int32_t* idx, int8_t* k_codes,
+                    float* k_scales, int8_t* v_codes, float* v_scales, int B, int Hkv, int M,
+                    int k, int d, int dtype, void* stream) {
+  return kv_quant_call(true, const_cast<void*>(k_src), const_cast<void*>(v_src), idx,
+                       CacheQ8{k_codes, k_scales, v_codes, v_scales}, B, Hkv, M, k, d, dtype,
+                       stream);
+}
+
+int h2o_kv_dequantize(const int8_t* k_codes, const float* k_scales, const int8_t* v_codes,
+                      const float* v_scales, const int32_t* idx, void* k_dst, void* v_dst, int B,
+                      int Hkv, int M, int k, int d, int dtype, void* stream) {
+  return kv_quant_call(false, k_dst, v_dst, idx,
+                       CacheQ8{const_cast<int8_t*>(k_codes), const_cast<float*>(k_scales),
+                               const_cast<int8_t*>(v_codes), const_cast<float*>(v_scales)},
+                       B, Hkv, M, k, d, dtype, stream);
+}
+
+size_t h2o_q8_workspace_bytes(int B, int Hq, int Hkv, int T, int M, int d, int dtype, int policy) {
+  if (dtype != H2O_F32 && dtype != H2O_BF16) return 0;
+  if (policy != H2O_POLICY_H2O && policy != H2O_POLICY_NORM && policy != H2O_POLICY_ORIG) return 0;
+  if (check_flash_shape(B, Hq, Hkv, T, M, d) != H2O_OK) return 0;
+  return attend_q8_bytes(B, Hq, Hkv, T, M, d, dtype) + evict_workspace(B, Hkv, M, T, policy);
+}
+
+int h2o_sdpa_chunk_q8(const void* q, const int8_t* k_codes, const float* k_scales,
+                      const int8_t* v_codes, const float* v_scales, const void* k_new,
+                      const void* v_new, void* out, float* lse, float* wsum, void* workspace,
+                      size_t workspace_bytes, int B, int Hq, int Hkv, int T, int M, int d,
+                      float scale, int dtype, void* stream) {
+  const CacheQ8 c{const_cast<int8_t*>(k_codes), const_cast<float*>(k_scales),
+                  const_cast<int8_t*>(v_codes), const_cast<float*>(v_scales)};
+  int rc = check_attend_q8(q, c, k_new, v_new, out, lse, wsum, workspace, workspace_bytes, B, Hq,
+                           Hkv, T, M, d, scale, dtype, 0);
+  if (!rc) rc = check_device();
+  if (rc) return rc;
+  return launched(launch_attend_q8(q, c, k_new, v_new, out, lse, wsum,
+                                   reinterpret_cast<char*>(workspace), B, Hq, Hkv, T, M, d, scale,
+                                   dtype, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int h2o_evict_insert_q8(int8_t* k_codes, float* k_scales, int8_t* v_codes, float* v_scales,
+                        float* scores, int32_t* token_pos, const void* k_new, const void* v_new,
+                        const float* wsum, int32_t* evict_idx, int B, int Hkv, int M, int T, int d,
+                        int k, int32_t pos0, int dtype, int policy, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  const CacheQ8 c{k_codes, k_scales, v_codes, v_scales};
+  int rc = check_evict_q8(c, scores, token_pos, k_new, v_new, wsum, evict_idx, B, Hkv, M, T, d, k,
+                          dtype, policy);
+  if (rc) return rc;
+  const size_t need = evict_workspace(B, Hkv, M, k, policy);
+  if (workspace_bytes < need || (need > 0 && !workspace))
+    return fail(H2O_EWORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, need);
+  if (!aligned16(workspace)) return fail(H2O_EALIGN, "workspace not 16-byte aligned");
+  rc = check_device();
+  if (rc) return rc;
+  return launched(launch_evict_q8(policy, c, scores, token_pos, k_new, v_new, wsum, evict_idx, B,
+                                  Hkv, M, T, d, k, pos0, pos0 + T, dtype == H2O_F32,
+                                  reinterpret_cast<char*>(workspace),
+                                  reinterpret_cast<hipStream_t>(stream)));
+}
+
+int h2o_chunk_step_q8(const void* q, int8_t* k_codes, float* k_scales, int8_t* v_codes,
+                      float* v_scales, float* scores, int32_t* token_pos, const void* k_new,
+                      const void* v_new, void* out, float* lse, float* wsum, int32_t* evict_idx,
+                      void* workspace, size_t workspace_bytes, int B, int Hq, int Hkv, int T,
+                      int M, int d, float scale, int32_t pos0, int dtype, int policy,
+                      void* stream) {
+  const CacheQ8 c{k_codes, k_scales, v_codes, v_scales};
+  if (dtype != H2O_F32 && dtype != H2O_BF16) return fail(H2O_EDTYPE, "dtype %d unknown", dtype);
+  int rc = check_flash_shape(B, Hq, Hkv, T, M, d);
+  if (!rc)
+    rc = check_evict_q8(c, scores, token_pos, k_new, v_new, wsum, evict_idx, B, Hkv, M, T, d, T,
+                        dtype, policy);
+  if (!rc)
+    rc = check_attend_q8(q, c, k_new, v_new, out, lse, wsum, workspace, workspace_bytes, B, Hq,
+                         Hkv, T, M, d, scale, dtype, evict_workspace(B, Hkv, M, T, policy));
+  if (!rc) rc = check_device();
+  if (rc) return rc;
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  char* ws = reinterpret_cast<char*>(workspace);
+  if (token_q8(Hq, Hkv, T, d, dtype) && policy == H2O_POLICY_H2O) {
+    const Shape s{B, Hq, Hkv, T, M, d};
+    return launched(launch_decode_step_q8(s, path_plan(s, 2), q, c, k_new, v_new, out, lse, wsum,
+                                          scores, token_pos, evict_idx, pos0, ws, scale, st));
+  }
+  hipError_t e = launch_attend_q8(q, c, k_new, v_new, out, lse, wsum, ws, B, Hq, Hkv, T, M, d,
+                                  scale, dtype, st);
+  if (e == hipSuccess) e = launch_accumulate(scores, wsum, B * Hkv, M, T, st);
+  if (e == hipSuccess)
+    e = launch_evict_q8(policy, c, scores, token_pos, k_new, v_new, wsum, evict_idx, B, Hkv, M, T,
+                        d, T, pos0, pos0 + T, dtype == H2O_F32,
+                        ws + attend_q8_bytes(B, Hq, Hkv, T, M, d, dtype), st);
+  return launched(e);
+}
+
+size_t h2o_tree_workspace_bytes(int B, int Hq, int Hkv, int T, int M, int d, int dtype) {
+  if (dtype != H2O_F32 && dtype != H2O_BF16) return 0;
+  if (check_flash_shape(B, Hq, Hkv, T, M, d) != H2O_OK) return 0;
+  return align256(flash_plan(FlashShape{B, Hq, Hkv, T, M, d, dtype == H2O_F32}, true).bytes);
+}
+
+int h2o_sdpa_tree(const void* q, const void* k_cache, const float* k_scales, const void* v_cache,
+                  const float* v_scales, const void* k_new, const void* v_new,
+                  const int32_t* parents, void* out, float* lse, void* workspace,
+                  size_t workspace_bytes, int B, int Hq, int Hkv, int T, int M, int d, float scale,
+                  int dtype, void* stream) {
+  int rc = check_tree(q, k_cache, k_scales, k_new, v_new, parents, workspace, workspace_bytes, B,
+                      Hq, Hkv, T, M, d, scale, dtype);
+  if (rc) return rc;
+  if (!out || !lse || (M > 0 && !v_cache)) return fail(H2O_EINVAL, "null tensor pointer");
+  if ((k_scales == nullptr) != (v_scales == nullptr))
+    return fail(H2O_EINVAL, "k_scales and v_scales go together (an 8-bit cache has both)");
+  if (!all_aligned({v_cache, v_scales, out, lse}))
+    return fail(H2O_EALIGN, "tensor pointer not 16-byte aligned");
+  rc = check_device();
+  if (rc) return rc;
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  char* ws = reinterpret_cast<char*>(workspace);
+  const FlashShape s{B, Hq, Hkv, T, M, d, dtype == H2O_F32};
+  const FlashPlan p = flash_plan(s, true);
+  const FlashIn in{k_scales != nullptr, q, k_cache, v_cache, k_scales, v_scales, k_new, v_new};
+  hipError_t e = launch_tree_bits(s, p, parents, ws, st);
+  if (e == hipSuccess)
+    e = (s.f32 ? launch_flash_f32 : launch_flash)(s, p, in, true, out, lse, ws, scale, st);
+  return launched(e);
+}
+
+int h2o_tree_accept(const void* q, const void* k_cache, const float* k_scales, const void* k_new,
+                    const void* v_new, const float* lse, const int32_t* path, void* k_acc,
+                    void* v_acc, float* wsum, void* workspace, size_t workspace_bytes, int B,
+                    int Hq, int Hkv, int T, int M, int A, int d, float scale, int dtype,
+                    void* stream) {
+  int rc = check_tree(q, k_cache, k_scales, k_new, v_new, path, workspace, workspace_bytes, B, Hq,
+                      Hkv, T, M, d, scale, dtype);
+  if (rc) return rc;
+  if (A < 1 || A > T) return fail(H2O_EINVAL, "path length A (%d) must be in [1, T = %d]", A, T);
+  if (!lse || !k_acc || !v_acc || !wsum) return fail(H2O_EINVAL, "null tensor pointer");
+  if (!all_aligned({lse, k_acc, v_acc, wsum}))
+    return fail(H2O_EALIGN, "tensor pointer not 16-byte aligned");
+  rc = check_device();
+  if (rc) return rc;
+  const FlashShape s{B, Hq, Hkv, T, M, d, dtype == H2O_F32};
+  FlashPlan p = flash_plan(s, true);
+  p.nranges = column_ranges(s, A);
+  const FlashIn in{k_scales != nullptr, q, k_cache, nullptr, k_scales, nullptr, k_new, v_new};
+  return launched((s.f32 ? launch_columns_f32 : launch_columns)(
+      s, p, in, lse, path, A, k_acc, v_acc, wsum, reinterpret_cast<char*>(workspace), scale,
+      reinterpret_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

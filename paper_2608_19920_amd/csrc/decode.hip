@@ -21,6 +21,7 @@
 // M, and a slot whose token position is later than the query's (pos0) is
 // masked; its stored logit is -inf.
 #include "internal.h"
+#include "q8.h"
 
 namespace h2o {
 namespace {
@@ -227,6 +228,47 @@ struct ScoreScan {
       }
   }
 };
+
+// The end of a split block, one barrier: every wave leaves its column statistics
+// and its unscaled O accumulators; then per head the common maximum over the
+// waves, each wave's weight, and the sums in wave order.
+template <int D, int G>
+__device__ __forceinline__ void split_merge(float m, float l, const f32x4 (&oacc)[D / 16],
+                                            float (*red_m)[16], float (*red_l)[16],
+                                            float (*ored)[G][D], int nsplit, int s, size_t bh,
+                                            float2* __restrict__ dstat, float* __restrict__ dO) {
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, grp = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  if (grp == 0) {
+    red_m[wave][col] = m;
+    red_l[wave][col] = l;
+  }
+  if (col < G) {
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) ored[wave][col][16 * db + 4 * grp + r] = oacc[db][r];
+  }
+  __syncthreads();
+  for (int c = tid; c < G * D; c += kThreads) {
+    const int g = c / D;
+    float mg = red_m[0][g];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) mg = fmaxf(mg, red_m[w][g]);
+    float a = 0.f, lt = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float mw = red_m[w][g];
+      const float sw = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - mg);
+      a += ored[w][g][c % D] * sw;
+      lt += red_l[w][g] * sw;
+    }
+    dO[(bh * nsplit + s) * (size_t)(G * D) + c] = a;
+    if (c % D == 0) dstat[(bh * nsplit + s) * G + g] = make_float2(mg, lt);
+  }
+}
 
 // NT: the K and V loads are non-temporal.
 template <int D, int G, bool CACHE, bool INS, bool NT>
@@ -447,38 +489,157 @@ __device__ __forceinline__ void split_body(
     if (!CACHE) __builtin_amdgcn_sched_barrier(0);
     consume(k + 1, 1);
   }
-  // block merge, one barrier: every wave leaves its column statistics and
-  // its unscaled O accumulators; then per head the common maximum over the
-  // waves, each wave's weight, and the sums in wave order
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
-  if (grp == 0) {
-    red_m[wave][col] = m;
-    red_l[wave][col] = l;
+  split_merge<D, G>(m, l, oacc, red_m, red_l, ored, nsplit, s, bh, dstat, dO);
+}
+
+// The split over an 8-bit cache (no token positions). A lane's 16 codes of K are
+// consecutive: element 64 x + 16 grp + u of its slot, and the queries are read in
+// the same order of d, which the sum does not depend on. Codes of V become bf16 on
+// their way through LDS. The step's 32 + 32 scales pass through LDS too: the key's
+// multiplies the logit, the value's the probability.
+template <int D, int G, bool NT>
+__device__ __forceinline__ void split_q8_body(
+    const bf16_t* __restrict__ q, const int8_t* __restrict__ kc, const float* __restrict__ ks,
+    const int8_t* __restrict__ vc, const float* __restrict__ vsc, int Hq, int Hkv, int M,
+    float c_log2, float* __restrict__ logits, float2* __restrict__ dstat,
+    float* __restrict__ dO, float* __restrict__ sink) {
+  constexpr int DX = D / 64;                 // 16-byte K loads per slot block
+  constexpr int NK = 2 * DX;
+  constexpr int RPL = 1024 / D;              // V rows per wave load
+  constexpr int NV = kStep / RPL;
+  constexpr int VP = vpitch<D>();
+  constexpr int kAux = NT ? 2 : 0;
+  __shared__ __attribute__((aligned(16))) bf16_t vs_all[kWaves][kStep * VP];
+  __shared__ __attribute__((aligned(16))) float sc_all[kWaves][2 * kStep];
+  __shared__ float red_m[kWaves][16], red_l[kWaves][16];
+  __shared__ float ored[kWaves][G][D];
+  const int s = blockIdx.x, nsplit = gridDim.x;
+  const size_t bh = blockIdx.y;
+  const int b = (int)(bh / Hkv), h = (int)(bh % Hkv);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, grp = lane >> 4;
+  const int head_steps = (M + kStep - 1) / kStep;
+  const int stream = s * kWaves + wave, nstreams = nsplit * kWaves;
+  const int nst = stream < head_steps ? (head_steps - stream + nstreams - 1) / nstreams : 0;
+  const __amdgpu_buffer_rsrc_t krs = buffer_rsrc(kc + bh * (size_t)M * D, (uint32_t)M * D);
+  const __amdgpu_buffer_rsrc_t vrs = buffer_rsrc(vc + bh * (size_t)M * D, (uint32_t)M * D);
+  const __amdgpu_buffer_rsrc_t ksr = buffer_rsrc(ks + bh * (size_t)M, (uint32_t)M * 4u);
+  const __amdgpu_buffer_rsrc_t vsr = buffer_rsrc(vsc + bh * (size_t)M, (uint32_t)M * 4u);
+  bf16_t* vs = vs_all[wave];
+  float* sc = sc_all[wave];
+  const int vrow = lane / (D / 16), vcol = 16 * (lane % (D / 16));
+  const uint32_t koff = (uint32_t)(col * D + 16 * grp);
+  const uint32_t voff = (uint32_t)(vrow * D + vcol);
+  float* lg_out = logits + (bh * G + col % G) * (size_t)logit_pitch(M);
+
+  u32x4 kr[2][NK], vr[2][NV];
+  float sk[2], sv[2];
+  auto issue = [&](int k, int u) {
+    const uint32_t slot0 = (uint32_t)((stream + k * nstreams) * kStep), base = slot0 * (uint32_t)D;
+    const int so = (int)((slot0 + (uint32_t)(lane & 31)) * 4u);
+    sk[u] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(ksr, so, 0, 0));
+    sv[u] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(vsr, so, 0, 0));
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int x = 0; x < DX; ++x)
+        kr[u][kb * DX + x] = __builtin_bit_cast(
+            u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                       krs, (int)(base + koff + (uint32_t)(16 * kb * D + 64 * x)), 0, kAux));
+#pragma unroll
+    for (int t = 0; t < NV; ++t)
+      vr[u][t] = __builtin_bit_cast(
+          u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                     vrs, (int)(base + voff + (uint32_t)(t * RPL * D)), 0, kAux));
+  };
+  bf16x8 qb[2 * DX];
+  {
+    const bf16_t* qrow = q + (size_t)(b * Hq + h * G + col % G) * D + 16 * grp;
+#pragma unroll
+    for (int x = 0; x < DX; ++x)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        qb[2 * x + u] = __builtin_bit_cast(bf16x8, load16(qrow + 64 * x + 8 * u));
   }
-  if (col < G) {
+  float m = -INFINITY, l = 0.f;
+  f32x4 oacc[D / 16];
 #pragma unroll
-    for (int db = 0; db < D / 16; ++db)
+  for (int db = 0; db < D / 16; ++db) oacc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  auto consume = [&](int k, int u) {
+    const int key0 = (stream + k * nstreams) * kStep;
+    sc[lane] = lane < kStep ? sk[u] * c_log2 : sv[u];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) ored[wave][col][16 * db + 4 * grp + r] = oacc[db][r];
-  }
-  __syncthreads();
-  for (int c = tid; c < G * D; c += kThreads) {
-    const int g = c / D;
-    float mg = red_m[0][g];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) mg = fmaxf(mg, red_m[w][g]);
-    float a = 0.f, lt = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float mw = red_m[w][g];
-      const float sw = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - mg);
-      a += ored[w][g][c % D] * sw;
-      lt += red_l[w][g] * sw;
+    for (int t = 0; t < NV; ++t) {
+      bf16x8* dst = reinterpret_cast<bf16x8*>(vs + (t * RPL + vrow) * VP + vcol);
+      dst[0] = q8::codes_bf16(vr[u][t][0], vr[u][t][1]);
+      dst[1] = q8::codes_bf16(vr[u][t][2], vr[u][t][3]);
     }
-    dO[(bh * nsplit + s) * (size_t)(G * D) + c] = a;
-    if (c % D == 0) dstat[(bh * nsplit + s) * G + g] = make_float2(mg, lt);
+    f32x4 sacc[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      sacc[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < DX; ++x) {
+        const u32x4 v = kr[u][kb * DX + x];
+        sacc[kb] = mfma(q8::codes_bf16(v[0], v[1]), qb[2 * x], sacc[kb]);
+        sacc[kb] = mfma(q8::codes_bf16(v[2], v[3]), qb[2 * x + 1], sacc[kb]);
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+    f32x4 cks[2], cvs[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      cks[kb] = *reinterpret_cast<const f32x4*>(sc + 16 * kb + 4 * grp);
+      cvs[kb] = *reinterpret_cast<const f32x4*>(sc + kStep + 16 * kb + 4 * grp);
+    }
+    float lg[8], mx = -INFINITY;
+    const bool tail = key0 + kStep > M;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      lg[i] = sacc[i >> 2][i & 3] * cks[i >> 2][i & 3];
+      if (tail && key0 + 16 * (i >> 2) + 4 * grp + (i & 3) >= M) lg[i] = -INFINITY;
+      mx = fmaxf(mx, lg[i]);
+    }
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      const int k4 = key0 + 16 * kb + 4 * grp;
+      float* dst = k4 < M ? lg_out + k4 : sink + 4 * lane;
+      *reinterpret_cast<f32x4*>(dst) =
+          f32x4{lg[4 * kb], lg[4 * kb + 1], lg[4 * kb + 2], lg[4 * kb + 3]};
+    }
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    if (__builtin_amdgcn_ballot_w64(mx > m + 64.f)) {
+      const bool up = mx > m + 64.f;
+      const float f = up ? __builtin_amdgcn_exp2f(m - mx) : 1.f;
+      l *= f;
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) oacc[db] *= f;
+      m = up ? mx : m;
+    }
+    bf16x8 pb;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int key = key0 + 16 * (i >> 2) + 4 * grp + (i & 3);
+      const float p = key < M ? __builtin_amdgcn_exp2f(lg[i] - m) : 0.f;
+      l += p;
+      pb[i] = (__bf16)(p * cvs[i >> 2][i & 3]);
+    }
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) oacc[db] = mfma(v_operand<D>(vs, db, lane), pb, oacc[db]);
+  };
+  issue(0, 0);
+  for (int k = 0; k < nst; k += 2) {   // whole trips of two steps, as in split_body
+    issue(k + 1, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    consume(k, 0);
+    issue(k + 2, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    consume(k + 1, 1);
   }
+  split_merge<D, G>(m, l, oacc, red_m, red_l, ored, nsplit, s, bh, dstat, dO);
 }
 
 // Register budgets at d = 64, where the kernels fit them without spilling:
@@ -507,10 +668,19 @@ void decode_split_ins(H2O_SPLIT_PARAMS) {
                                ins);
 }
 #undef H2O_SPLIT_PARAMS
+template <int D, int G, bool NT>
+__global__ __launch_bounds__(kThreads) void decode_split_q8(
+    const bf16_t* __restrict__ q, const int8_t* __restrict__ kc, const float* __restrict__ ks,
+    const int8_t* __restrict__ vc, const float* __restrict__ vs, int Hq, int Hkv, int M,
+    float c_log2, float* __restrict__ logits, float2* __restrict__ dstat, float* __restrict__ dO,
+    float* __restrict__ sink) {
+  split_q8_body<D, G, NT>(q, kc, ks, vc, vs, Hq, Hkv, M, c_log2, logits, dstat, dO, sink);
+}
 
-template <int D, int G, bool CACHE, bool INS>
+template <int D, int G, bool CACHE, bool INS, bool Q8>
 const void* split_kernel() {
-  if constexpr (INS) return reinterpret_cast<const void*>(decode_split_ins<D, G, false>);
+  if constexpr (Q8) return reinterpret_cast<const void*>(decode_split_q8<D, G, false>);
+  else if constexpr (INS) return reinterpret_cast<const void*>(decode_split_ins<D, G, false>);
   else if constexpr (CACHE) return reinterpret_cast<const void*>(decode_split_cache<D, G, false>);
   else return reinterpret_cast<const void*>(decode_split<D, G, false>);
 }
@@ -579,7 +749,7 @@ __device__ __forceinline__ void head_stats_from(HeadStats& hs, const StatIn<D>& 
     if (has_chunk) L += __builtin_amdgcn_exp2f(lnew - mx);
     if (lane < nsplit) hs.wt[lane * G + g] = wt;
     if (lane == 0) {
-      const bool any = L > 0.f;
+      const bool any = L != 0.f;   // (a NaN, of a row of an 8-bit cache, stays one)
       const float lm = any ? mx + __log2f(L) : INFINITY;
       hs.lnew[g] = lnew;
       hs.lam[g] = lm;
@@ -750,10 +920,32 @@ __global__ __launch_bounds__(kCombThreads) void decode_combine(
   }
 }
 
+// One wave: the row whose elements 8 lane .. +7 lane < D / 8 has in v goes into an
+// 8-bit cache.
+__device__ __forceinline__ void put_row_q8(int8_t* codes, float* scales, size_t slot, int D,
+                                           const u32x4& v, int lane) {
+  float x[8];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    x[2 * w] = __uint_as_float(v[w] << 16);
+    x[2 * w + 1] = __uint_as_float(v[w] & 0xFFFF0000u);
+  }
+  // lanes past the row hold zeros
+  const float sc = q8::row_scale(q8::lanes_max<16>(q8::amax_bits<8>(x)));
+  uint32_t c[2];
+  q8::quantize<8>(x, sc, c);
+  if (lane < D / 8) {
+    *reinterpret_cast<uint2*>(codes + slot * D + 8 * lane) = make_uint2(c[0], c[1]);
+    if (lane == 0) scales[slot] = sc;
+  }
+}
+
 // The end of a token step whose combine ran with CAND: one wave per head takes
 // the smallest of the blocks' candidates and inserts the chunk there.
+// Q8: the rows go into an 8-bit cache (c8; kc and vc are not used).
+template <bool Q8>
 __global__ __launch_bounds__(64) void decode_insert(
-    bf16_t* __restrict__ kc, bf16_t* __restrict__ vc, const bf16_t* __restrict__ kn,
+    bf16_t* __restrict__ kc, bf16_t* __restrict__ vc, CacheQ8 c8, const bf16_t* __restrict__ kn,
     const bf16_t* __restrict__ vn, int D, int M, int nx, const uint2* __restrict__ cand,
     const float* __restrict__ wsum, float* __restrict__ scores, int32_t* __restrict__ token_pos,
     int32_t* __restrict__ evict_idx, int32_t pos0) {
@@ -778,7 +970,10 @@ __global__ __launch_bounds__(64) void decode_insert(
     scores[slot] = wnew;
     if (token_pos) token_pos[slot] = pos0;
   }
-  if (copy) {
+  if constexpr (Q8) {
+    put_row_q8(c8.k, c8.ks, slot, D, krow, lane);
+    put_row_q8(c8.v, c8.vs, slot, D, vrow, lane);
+  } else if (copy) {
     *reinterpret_cast<u32x4*>(kc + slot * D + 8 * lane) = krow;
     *reinterpret_cast<u32x4*>(vc + slot * D + 8 * lane) = vrow;
   }
@@ -806,9 +1001,10 @@ constexpr int kFinSlots = kFinThreads * kFinVec;    // slots of a head, at most
 // Blocks x < heads do the slots of head x, blocks heads + x its out and lse;
 // with OUT false (the eviction half of a step, whose attend call wrote out and
 // lse by decode_combine) there are only the former.
-template <int D, int G, bool OUT>
+// Q8: the chunk goes into an 8-bit cache (c8; kc and vc are not used).
+template <int D, int G, bool OUT, bool Q8 = false>
 __global__ __launch_bounds__(kFinThreads) void decode_finish(
-    const bf16_t* __restrict__ q, bf16_t* __restrict__ kc, bf16_t* __restrict__ vc,
+    const bf16_t* __restrict__ q, bf16_t* __restrict__ kc, bf16_t* __restrict__ vc, CacheQ8 c8,
     const bf16_t* __restrict__ kn, const bf16_t* __restrict__ vn, int heads, int Hq, int Hkv,
     int M, int nsplit, float c_log2, const float* __restrict__ logits,
     const float2* __restrict__ dstat, const float* __restrict__ dO, bf16_t* __restrict__ out,
@@ -919,7 +1115,12 @@ __global__ __launch_bounds__(kFinThreads) void decode_finish(
     evict_idx[bh] = slot;
     if (token_pos) token_pos[bh * M + slot] = pos0;
   }
-  if (tid < D / 8) {
+  if constexpr (Q8) {
+    if (wave == 0) {
+      put_row_q8(c8.k, c8.ks, bh * M + slot, D, krow, lane);
+      put_row_q8(c8.v, c8.vs, bh * M + slot, D, vrow, lane);
+    }
+  } else if (tid < D / 8) {
     reinterpret_cast<u4*>(kc + (bh * M + slot) * (size_t)D)[tid] = krow;
     reinterpret_cast<u4*>(vc + (bh * M + slot) * (size_t)D)[tid] = vrow;
   }
@@ -929,12 +1130,12 @@ __global__ __launch_bounds__(kFinThreads) void decode_finish(
 // once (blocks per CU of this kernel instance x CUs), at most kMaxSplit and
 // at most one wave per step of slots. (The non-temporal kernels take the same
 // registers and LDS, so the same count.)
-template <int D, int G, bool CACHE, bool INS = false>
+template <int D, int G, bool CACHE, bool INS = false, bool Q8 = false>
 int split_count(int M, int BH) {
   static int resident = 0;
   if (!resident) {
     int per_cu = 0, dev = 0, cus = 0;
-    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, split_kernel<D, G, CACHE, INS>(),
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, split_kernel<D, G, CACHE, INS, Q8>(),
                                                      kThreads, 0) != hipSuccess || per_cu < 1)
       per_cu = 2;
     if (hipGetDevice(&dev) != hipSuccess ||
@@ -1103,25 +1304,28 @@ namespace {
 hipError_t launch_finish(const Shape& s, const Plan& p, bool out_too, int ns, const void* q,
                          void* kc, void* vc, const void* kn, const void* vn, void* out,
                          float* lse, float* wsum, float* scores, int32_t* token_pos,
-                         int32_t* evict_idx, int32_t pos0, char* ws, float c, hipStream_t st) {
+                         int32_t* evict_idx, int32_t pos0, char* ws, float c, hipStream_t st,
+                         const CacheQ8* c8 = nullptr) {
+  const CacheQ8 to = c8 ? *c8 : CacheQ8{};
   if (s.M > kFinSlots) {
     const hipError_t e = launch_combine(s, p, ns, q, kn, vn, out_too ? out : nullptr, lse, wsum,
                                         scores, nullptr, true, ws, c, st);
     if (e != hipSuccess) return e;
-    return launch_kernel(K_DECODE_INSERT, decode_insert, dim3(s.BH()), dim3(64), st, (bf16_t*)kc,
-                         (bf16_t*)vc, (const bf16_t*)kn, (const bf16_t*)vn, s.d, s.M,
+    return launch_kernel(K_DECODE_INSERT, c8 ? decode_insert<true> : decode_insert<false>,
+                         dim3(s.BH()), dim3(64), st, (bf16_t*)kc, (bf16_t*)vc, to, (const bf16_t*)kn, (const bf16_t*)vn, s.d, s.M,
                          (s.M + kCombSlots - 1) / kCombSlots, (const uint2*)(ws + p.off_keys),
                          (const float*)wsum, scores, token_pos, evict_idx, pos0);
   }
   auto go = [&](auto kern) {
     return launch_kernel(K_DECODE_FINISH, kern, dim3(out_too ? 2 * s.BH() : s.BH()),
-                         dim3(kFinThreads), st, (const bf16_t*)q, (bf16_t*)kc, (bf16_t*)vc,
+                         dim3(kFinThreads), st, (const bf16_t*)q, (bf16_t*)kc, (bf16_t*)vc, to,
                          (const bf16_t*)kn, (const bf16_t*)vn, s.BH(), s.Hq, s.Hkv, s.M, ns, c,
                          (const float*)(ws + p.off_logits), (const float2*)(ws + p.off_stats),
                          (const float*)(ws + p.off_opart), (bf16_t*)out, lse, wsum, scores,
                          token_pos, evict_idx, pos0);
   };
   return with_shape(s, [&](auto d, auto g) {
+    if (c8) return go(decode_finish<d.value, g.value, true, true>);
     return out_too ? go(decode_finish<d.value, g.value, true>)
                    : go(decode_finish<d.value, g.value, false>);
   });
@@ -1168,6 +1372,53 @@ hipError_t launch_decode_step(const Shape& s, const Plan& p, const void* q, void
   if (e != hipSuccess) return e;
   return launch_finish(s, p, true, ns, q, kc, vc, kn, vn, out, lse, wsum, scores, token_pos,
                        evict_idx, pos0, ws, c, st);
+}
+
+namespace {
+
+// The split over an 8-bit cache; the split count in *ns.
+hipError_t launch_decode_split_q8(const Shape& s, const Plan& p, const void* q, const CacheQ8& c8,
+                                  char* ws, float c, hipStream_t st, int* ns) {
+  *ns = 0;
+  if (s.M == 0) return hipSuccess;
+  return with_shape(s, [&](auto d, auto g) {
+    constexpr int D = decltype(d)::value, G = decltype(g)::value;
+    *ns = split_count<D, G, false, false, true>(s.M, s.BH());
+    const bool nt = (size_t)s.BH() * s.M * (size_t)(2 * D) >= kNtBytes;
+    return launch_kernel(K_DECODE_SPLIT, nt ? decode_split_q8<D, G, true> : decode_split_q8<D, G, false>,
+                         dim3(*ns, s.BH()), dim3(kThreads), st, (const bf16_t*)q,
+                         (const int8_t*)c8.k, (const float*)c8.ks, (const int8_t*)c8.v,
+                         (const float*)c8.vs, s.Hq, s.Hkv, s.M, c,
+                         reinterpret_cast<float*>(ws + p.off_logits),
+                         reinterpret_cast<float2*>(ws + p.off_stats),
+                         reinterpret_cast<float*>(ws + p.off_opart),
+                         reinterpret_cast<float*>(ws + p.off_parts));
+  });
+}
+
+}  // namespace
+
+hipError_t launch_sdpa_decode_q8(const Shape& s, const Plan& p, const void* q, const CacheQ8& c8,
+                                 const void* kn, const void* vn, void* out, float* lse,
+                                 float* wsum, char* ws, float scale, hipStream_t st) {
+  const float c = scale * kLog2e;
+  int ns = 0;
+  const hipError_t e = launch_decode_split_q8(s, p, q, c8, ws, c, st, &ns);
+  if (e != hipSuccess) return e;
+  return launch_combine(s, p, ns, q, kn, vn, out, lse, wsum, nullptr, nullptr, false, ws, c, st);
+}
+
+hipError_t launch_decode_step_q8(const Shape& s, const Plan& p, const void* q, const CacheQ8& c8,
+                                 const void* kn, const void* vn, void* out, float* lse,
+                                 float* wsum, float* scores, int32_t* token_pos,
+                                 int32_t* evict_idx, int32_t pos0, char* ws, float scale,
+                                 hipStream_t st) {
+  const float c = scale * kLog2e;
+  int ns = 0;
+  const hipError_t e = launch_decode_split_q8(s, p, q, c8, ws, c, st, &ns);
+  if (e != hipSuccess) return e;
+  return launch_finish(s, p, true, ns, q, nullptr, nullptr, kn, vn, out, lse, wsum, scores,
+                       token_pos, evict_idx, pos0, ws, c, st, &c8);
 }
 
 }  // namespace h2o

@@ -45,6 +45,9 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
+template <int V>
+struct IntConst { static constexpr int value = V; };
+
 // ----------------------------------------------------------- problem shape
 // Two arrangements of the keys a chunk attends:
 //  - chunk mode: [M cache slots, all visible || the T chunk keys, causal], the
@@ -135,7 +138,8 @@ enum KernelId {
   K_GENERIC_LSE = 0, K_GENERIC_MAIN, K_MFMA_LSE, K_MFMA_MAIN, K_SPLIT_REDUCE, K_COLSUM_REDUCE,
   K_ACCUMULATE, K_BOTTOMK, K_INSERT, K_DECODE_SPLIT, K_DECODE_COMBINE, K_ARGMIN_INSERT,
   K_DECODE_FINISH, K_KEYS, K_BWD_DQ, K_BWD_DKDV, K_KV_COPY, K_BWD_DOT, K_BWD_DQ_REDUCE,
-  K_BOTTOMK_INSERT, K_F32_ATTEND, K_DECODE_INSERT, K_COUNT
+  K_BOTTOMK_INSERT, K_F32_ATTEND, K_DECODE_INSERT, K_KV_QUANT, K_FLASH, K_FLASH_COMBINE,
+  K_COLUMNS, K_COLUMN_REDUCE, K_TREE_BITS, K_COUNT
 };
 // While timing is switched on (h2o_debug_timing), kernels go out through
 // hipExtLaunchKernel with a start and a stop event: the runtime stamps them
@@ -289,5 +293,79 @@ hipError_t launch_sdpa_backward_mfma(const Shape& s, const void* q, const void* 
 // (scatter), `vecs` 16-byte vectors per cache row.
 hipError_t launch_kv_copy(bool gather, void* cache, const int32_t* idx, void* rows, int nrows,
                           int M, int k, int vecs, hipStream_t st);
+
+// ------------------------------------------------------- 8-bit cache and tree
+// K and V rows as codes [BH][M][d] with a scale each [BH][M] (q8.h).
+struct CacheQ8 {
+  int8_t* k;
+  float* ks;
+  int8_t* v;
+  float* vs;
+};
+// Rows i < k of each of `rows` heads go to slot idx[row, i] (idx null: slot i);
+// slots outside [0, M) are skipped. scores non-null: the insert of an eviction as
+// well (the slot's score becomes wsum[row, M + i], row pitch M + T, its position
+// pos0 + i). rows * k < 2^28.
+hipError_t launch_kv_quantize(const void* k_src, const void* v_src, const int32_t* idx,
+                              const CacheQ8& c, int rows, int M, int k, int d, bool f32,
+                              hipStream_t st, float* scores = nullptr,
+                              int32_t* token_pos = nullptr, const float* wsum = nullptr,
+                              int T = 0, int32_t pos0 = 0);
+hipError_t launch_kv_dequantize(const CacheQ8& c, const int32_t* idx, void* k_dst, void* v_dst,
+                                int rows, int M, int k, int d, bool f32, hipStream_t st);
+
+// Attention of T rows per query head over [M slots || T chunk keys] in one sweep,
+// and column sums in a second one (flash.hip, flash_f32.hip).
+struct FlashShape {
+  int B, Hq, Hkv, T, M, d;
+  bool f32;
+  int G() const { return Hq / Hkv; }
+  int BH() const { return B * Hkv; }
+};
+struct FlashIn {
+  bool q8;                      // the cache is in 8 bits
+  const void *q, *kc, *vc;
+  const float *ks, *vs;
+  const void *kn, *vn;
+};
+struct FlashPlan {
+  int rows;                     // packed rows per block
+  int nsplit;                   // key ranges
+  int nranges;                  // row ranges of the column sums
+  size_t off_stats, off_opart, off_bits, off_parts, bytes;
+};
+constexpr int kMaxFlashSplit = 32, kMaxColumnRanges = 8;
+constexpr int kColumnKeys = 128, kColumnKeysF32 = 64;   // keys per block of the column sums
+FlashPlan flash_plan(const FlashShape& s, bool tree);
+int column_ranges(const FlashShape& s, int ncol);
+// tree: the mask of the ancestor bits that launch_tree_bits left in ws.
+hipError_t launch_flash(const FlashShape& s, const FlashPlan& p, const FlashIn& in, bool tree,
+                        void* out, float* lse, char* ws, float scale, hipStream_t st);
+hipError_t launch_flash_f32(const FlashShape& s, const FlashPlan& p, const FlashIn& in, bool tree,
+                            void* out, float* lse, char* ws, float scale, hipStream_t st);
+hipError_t launch_flash_combine(const FlashShape& s, const FlashPlan& p, void* out, float* lse,
+                                const char* ws, hipStream_t st);
+hipError_t launch_tree_bits(const FlashShape& s, const FlashPlan& p, const int32_t* parents,
+                            char* ws, hipStream_t st);
+// path null: wsum [BH][M + T] of all rows of the chunk, causal; else [BH][M + A] of
+// the path's A nodes, and their keys and values into k_acc and v_acc.
+hipError_t launch_columns(const FlashShape& s, const FlashPlan& p, const FlashIn& in,
+                          const float* lse, const int32_t* path, int A, void* k_acc, void* v_acc,
+                          float* wsum, char* ws, float scale, hipStream_t st);
+hipError_t launch_columns_f32(const FlashShape& s, const FlashPlan& p, const FlashIn& in,
+                              const float* lse, const int32_t* path, int A, void* k_acc,
+                              void* v_acc, float* wsum, char* ws, float scale, hipStream_t st);
+hipError_t launch_column_reduce(const float* parts, float* wsum, size_t n, int nranges,
+                                hipStream_t st);
+// T == 1 over an 8-bit cache, bf16 queries, a plan of path 2: the attention with
+// the summed weights, and the whole step with the h2o ranking.
+hipError_t launch_sdpa_decode_q8(const Shape& s, const Plan& p, const void* q, const CacheQ8& c,
+                                 const void* kn, const void* vn, void* out, float* lse,
+                                 float* wsum, char* ws, float scale, hipStream_t st);
+hipError_t launch_decode_step_q8(const Shape& s, const Plan& p, const void* q, const CacheQ8& c,
+                                 const void* kn, const void* vn, void* out, float* lse,
+                                 float* wsum, float* scores, int32_t* token_pos,
+                                 int32_t* evict_idx, int32_t pos0, char* ws, float scale,
+                                 hipStream_t st);
 
 }  // namespace h2o

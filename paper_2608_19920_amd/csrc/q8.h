@@ -1,0 +1,126 @@
+// The 8-bit cache row (gfx950): d signed bytes and one float32 scale.
+//
+//   scale = max|x| / 127 (float32, correctly rounded), code = round(x / scale),
+//   ties to even, so |code| <= 127 and |x - code * scale| <= scale / 2.
+//
+// A row whose scale would be subnormal has scale 0 and codes 0; a row with an Inf
+// or NaN has scale NaN and codes 0, so it reads back as NaN and never as data.
+// A code is exact in bf16 (7 bits), so a matrix product over codes is as exact as
+// one over bf16 data; the scale of a key multiplies its column of scores, the
+// scale of a value its column of probabilities, both in float32.
+#pragma once
+
+#include "internal.h"
+
+namespace h2o {
+namespace q8 {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr uint32_t kInfBits = 0x7F800000u;
+
+__device__ __forceinline__ float code_f32(uint32_t w, int byte) {
+  return (float)(int8_t)(w >> (8 * byte));
+}
+// Eight codes (two words) as a bf16 matrix operand.
+__device__ __forceinline__ bf16x8 codes_bf16(uint32_t lo, uint32_t hi) {
+  bf16x8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r[i] = (__bf16)code_f32(lo, i);
+    r[4 + i] = (__bf16)code_f32(hi, i);
+  }
+  return r;
+}
+
+// Scale of a row from the bits of max|x| (as unsigned integers the finite
+// magnitudes come before Inf, and Inf before every NaN).
+__device__ __forceinline__ float row_scale(uint32_t amax_bits) {
+  if (amax_bits >= kInfBits) return __uint_as_float(0x7FC00000u);
+  const float s = __uint_as_float(amax_bits) / 127.f;
+  return s < 1.17549435e-38f ? 0.f : s;
+}
+
+// Codes of N values of a row of that scale. fma(x, 1/scale, 1.5 * 2^23) leaves
+// the rounded quotient in its low byte; 1/scale is off by half a unit, so a
+// quotient within 127 * 2^-24 of a border can come out one too far: the remainder
+// x - r * scale is exact (a multiple of scale's last bit below scale), and where
+// it reaches half a scale the code is settled by it. That is rare, so it is
+// tested for all N at once.
+template <int N>
+__device__ __forceinline__ void quantize(const float (&x)[N], float scale, uint32_t (&codes)[N / 4]) {
+  constexpr float kMagic = 12582912.f;   // 1.5 * 2^23
+  if (!(scale > 0.f)) {   // zeros, or a row with an Inf or NaN
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) codes[i] = 0u;
+    return;
+  }
+  const float inv = 1.f / scale;
+  float y[N], worst = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    y[i] = fmaf(x[i], inv, kMagic);
+    worst = fmaxf(worst, fabsf(fmaf(kMagic - y[i], scale, x[i])));
+  }
+  if (worst + worst >= scale) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float r = y[i] - kMagic, t = fmaf(-r, scale, x[i]), t2 = fabsf(t + t);
+      const bool odd = ((int)r & 1) != 0;
+      if (t2 > scale || (t2 == scale && odd)) y[i] += t > 0.f ? 1.f : -1.f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i)
+    codes[i] = (__float_as_uint(y[4 * i]) & 0xFFu) | ((__float_as_uint(y[4 * i + 1]) & 0xFFu) << 8) |
+               ((__float_as_uint(y[4 * i + 2]) & 0xFFu) << 16) |
+               (__float_as_uint(y[4 * i + 3]) << 24);
+}
+
+// N values of a row, 16-byte loads.
+template <int N>
+__device__ __forceinline__ void load_row(float (&x)[N], const bf16_t* p) {
+#pragma unroll
+  for (int i = 0; i < N / 8; ++i) {
+    const u32x4 v = reinterpret_cast<const u32x4*>(p)[i];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      x[8 * i + 2 * w] = __uint_as_float(v[w] << 16);
+      x[8 * i + 2 * w + 1] = __uint_as_float(v[w] & 0xFFFF0000u);
+    }
+  }
+}
+template <int N>
+__device__ __forceinline__ void load_row(float (&x)[N], const float* p) {
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) {
+    const f32x4 v = reinterpret_cast<const f32x4*>(p)[i];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) x[4 * i + w] = v[w];
+  }
+}
+template <int N>
+__device__ __forceinline__ uint32_t amax_bits(const float (&x)[N]) {
+  uint32_t m = 0u;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t a = __float_as_uint(x[i]) & 0x7FFFFFFFu;
+    m = a > m ? a : m;
+  }
+  return m;
+}
+// Maximum over the LANES lanes (a power of two) that share a row.
+template <int LANES>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t m) {
+#pragma unroll
+  for (int o = 1; o < LANES; o <<= 1) {
+    const uint32_t v = __shfl_xor(m, o, 64);
+    m = v > m ? v : m;
+  }
+  return m;
+}
+
+}  // namespace q8
+}  // namespace h2o

@@ -28,7 +28,10 @@ EXPORTED = ["h2o_workspace_bytes", "h2o_sdpa_chunk", "h2o_accumulate_scores",
             "h2o_noalloc_scratch_bytes", "h2o_chunk_step_noalloc",
             "h2o_cache_workspace_bytes", "h2o_sdpa_cache", "h2o_backward_workspace_bytes",
             "h2o_sdpa_chunk_backward", "h2o_kv_gather", "h2o_kv_scatter",
-            "h2o_chunk_step_insert_first", "h2o_bottomk", "h2o_last_error", "h2o_debug_force_path",
+            "h2o_chunk_step_insert_first", "h2o_kv_quantize", "h2o_kv_dequantize",
+            "h2o_q8_workspace_bytes", "h2o_sdpa_chunk_q8", "h2o_evict_insert_q8",
+            "h2o_chunk_step_q8", "h2o_tree_workspace_bytes", "h2o_sdpa_tree", "h2o_tree_accept",
+            "h2o_bottomk", "h2o_last_error", "h2o_debug_force_path",
             "h2o_debug_timing", "h2o_debug_kernel_time", "h2o_version"]
 KERNEL_IDS = {"generic_lse": 0, "generic_main": 1, "mfma_lse": 2, "mfma_main": 3,
               "split_reduce": 4, "colsum_reduce": 5, "accumulate": 6, "bottomk": 7,
@@ -36,7 +39,8 @@ KERNEL_IDS = {"generic_lse": 0, "generic_main": 1, "mfma_lse": 2, "mfma_main": 3
               "argmin_insert": 11, "decode_finish": 12, "variant_keys": 13,
               "bwd_dq": 14, "bwd_dkdv": 15, "kv_copy": 16, "bwd_dot": 17,
               "bwd_dq_reduce": 18, "bottomk_insert": 19, "f32_attend": 20,
-              "decode_insert": 21}
+              "decode_insert": 21, "kv_quant": 22, "flash": 23, "flash_combine": 24,
+              "columns": 25, "column_reduce": 26, "tree_bits": 27}
 # eviction rankings (Sec. "Variants of Heavy-Hitter Oracle"), as h2o_policy
 POLICIES = {"h2o": 0, "h2o_norm": 1, "h2o_orig": 2}
 
@@ -97,6 +101,24 @@ def lib() -> ctypes.CDLL:
     for name in ("h2o_kv_gather", "h2o_kv_scatter"):
         getattr(L, name).argtypes = [vp] * 3 + [i] * 6 + [vp]
         getattr(L, name).restype = i
+    L.h2o_kv_quantize.argtypes = [vp] * 7 + [i] * 6 + [vp]
+    L.h2o_kv_quantize.restype = i
+    L.h2o_kv_dequantize.argtypes = [vp] * 7 + [i] * 6 + [vp]
+    L.h2o_kv_dequantize.restype = i
+    L.h2o_q8_workspace_bytes.argtypes = [i] * 8
+    L.h2o_q8_workspace_bytes.restype = sz
+    L.h2o_sdpa_chunk_q8.argtypes = [vp] * 11 + [sz] + [i] * 6 + [f, i, vp]
+    L.h2o_sdpa_chunk_q8.restype = i
+    L.h2o_evict_insert_q8.argtypes = [vp] * 10 + [i] * 6 + [ctypes.c_int32, i, i, vp, sz, vp]
+    L.h2o_evict_insert_q8.restype = i
+    L.h2o_chunk_step_q8.argtypes = [vp] * 14 + [sz] + [i] * 6 + [f, ctypes.c_int32, i, i, vp]
+    L.h2o_chunk_step_q8.restype = i
+    L.h2o_tree_workspace_bytes.argtypes = [i] * 7
+    L.h2o_tree_workspace_bytes.restype = sz
+    L.h2o_sdpa_tree.argtypes = [vp] * 11 + [sz] + [i] * 6 + [f, i, vp]
+    L.h2o_sdpa_tree.restype = i
+    L.h2o_tree_accept.argtypes = [vp] * 11 + [sz] + [i] * 7 + [f, i, vp]
+    L.h2o_tree_accept.restype = i
     L.h2o_bottomk.argtypes = [vp, i, i, i, vp, vp]
     L.h2o_bottomk.restype = i
     L.h2o_last_error.argtypes = []
@@ -485,6 +507,224 @@ def h2o_kv_scatter(cache, idx, src, stream=None) -> None:
                                 B, Hkv, M, k, d, _dtype_code(cache), _stream(stream)))
 
 
+# ------------------------------------------------- the cache in 8 bits
+def _q8_cache(k_codes, k_scales, v_codes, v_scales):
+    """(B, Hkv, M, d) of an 8-bit cache."""
+    B, Hkv, M, d = k_codes.shape
+    if k_codes.dtype != torch.int8 or v_codes.dtype != torch.int8:
+        raise TypeError("codes must be int8")
+    if v_codes.shape != (B, Hkv, M, d):
+        raise ValueError("v_codes must be [B,Hkv,M,d] like k_codes")
+    for name, t in (("k_scales", k_scales), ("v_scales", v_scales)):
+        if t.shape != (B, Hkv, M) or t.dtype != torch.float32:
+            raise ValueError(f"{name} must be float32 [B,Hkv,M]")
+    return B, Hkv, M, d
+
+
+def _q8_ptrs(k_codes, k_scales, v_codes, v_scales):
+    return (_dev(k_codes, "k_codes"), _dev(k_scales, "k_scales"), _dev(v_codes, "v_codes"),
+            _dev(v_scales, "v_scales"))
+
+
+def _q8_rows(k_rows, v_rows, idx, B, Hkv, M, d):
+    k = k_rows.shape[2]
+    if k_rows.shape != (B, Hkv, k, d) or v_rows.shape != (B, Hkv, k, d) or \
+            v_rows.dtype != k_rows.dtype:
+        raise ValueError("rows of K and V must be [B,Hkv,k,d] of one dtype")
+    if idx is not None and (idx.dtype != torch.int32 or idx.shape != (B, Hkv, k)):
+        raise ValueError("idx must be int32 [B,Hkv,k]")
+    return k
+
+
+def h2o_kv_quantize(k_src, v_src, k_codes, k_scales, v_codes, v_scales, idx=None,
+                    stream=None) -> None:
+    """Rows k_src, v_src [B,Hkv,k,d] into an 8-bit cache (codes int8 [B,Hkv,M,d],
+    scales f32 [B,Hkv,M]): row i to slot idx[b,h,i], or to slot i without idx."""
+    B, Hkv, M, d = _q8_cache(k_codes, k_scales, v_codes, v_scales)
+    k = _q8_rows(k_src, v_src, idx, B, Hkv, M, d)
+    _check(lib().h2o_kv_quantize(
+        _dev(k_src, "k_src"), _dev(v_src, "v_src"), _dev(idx, "idx"),
+        *_q8_ptrs(k_codes, k_scales, v_codes, v_scales), B, Hkv, M, k, d, _dtype_code(k_src),
+        _stream(stream)))
+
+
+def h2o_kv_dequantize(k_codes, k_scales, v_codes, v_scales, k_dst, v_dst, idx=None,
+                      stream=None) -> None:
+    """The values of slot idx[b,h,i] (slot i without idx) into k_dst, v_dst
+    [B,Hkv,k,d], rounded to their dtype."""
+    B, Hkv, M, d = _q8_cache(k_codes, k_scales, v_codes, v_scales)
+    k = _q8_rows(k_dst, v_dst, idx, B, Hkv, M, d)
+    _check(lib().h2o_kv_dequantize(
+        *_q8_ptrs(k_codes, k_scales, v_codes, v_scales), _dev(idx, "idx"), _dev(k_dst, "k_dst"),
+        _dev(v_dst, "v_dst"), B, Hkv, M, k, d, _dtype_code(k_dst), _stream(stream)))
+
+
+def h2o_q8_workspace_bytes(B, Hq, Hkv, T, M, d, dtype, policy="h2o") -> int:
+    code = dtype if isinstance(dtype, int) else _dtype_code(torch.empty(0, dtype=dtype))
+    return int(lib().h2o_q8_workspace_bytes(B, Hq, Hkv, T, M, d, code, _policy_code(policy)))
+
+
+def _chunk_q8(q, k_codes, k_scales, v_codes, v_scales, k_new, v_new, out, lse, wsum):
+    B, Hq, T, d = q.shape
+    if _q8_cache(k_codes, k_scales, v_codes, v_scales) != (B, k_codes.shape[1],
+                                                           k_codes.shape[2], d):
+        raise ValueError("cache shape mismatch")
+    Hkv, M = k_codes.shape[1], k_codes.shape[2]
+    for name, t, shape in (("k_new", k_new, (B, Hkv, T, d)), ("v_new", v_new, (B, Hkv, T, d)),
+                           ("out", out, (B, Hq, T, d))):
+        if t.dtype != q.dtype:
+            raise TypeError(f"{name} dtype {t.dtype} != q dtype {q.dtype}")
+        if t.shape != shape:
+            raise ValueError(f"{name} shape mismatch")
+    if lse.shape != (B, Hq, T) or lse.dtype != torch.float32:
+        raise ValueError("lse must be float32 [B,Hq,T]")
+    if wsum.shape != (B, Hkv, M + T) or wsum.dtype != torch.float32:
+        raise ValueError("wsum must be float32 [B,Hkv,M+T]")
+    return B, Hq, Hkv, T, M, d
+
+
+def _nbytes(workspace) -> int:
+    return workspace.numel() * workspace.element_size() if workspace is not None else 0
+
+
+def h2o_sdpa_chunk_q8(q, k_codes, k_scales, v_codes, v_scales, k_new, v_new, out, lse, wsum,
+                      workspace, scale: Optional[float] = None, stream=None) -> None:
+    """h2o_sdpa_chunk over an 8-bit cache; workspace uint8 of
+    h2o_q8_workspace_bytes(...) bytes."""
+    sizes = _chunk_q8(q, k_codes, k_scales, v_codes, v_scales, k_new, v_new, out, lse, wsum)
+    if scale is None:
+        scale = sizes[-1] ** -0.5
+    _check(lib().h2o_sdpa_chunk_q8(
+        _dev(q, "q"), *_q8_ptrs(k_codes, k_scales, v_codes, v_scales), _dev(k_new, "k_new"),
+        _dev(v_new, "v_new"), _dev(out, "out"), _dev(lse, "lse"), _dev(wsum, "wsum"),
+        _dev(workspace, "workspace"), _nbytes(workspace), *sizes, float(scale), _dtype_code(q),
+        _stream(stream)))
+
+
+def _evict_q8(scores, token_pos, evict_idx, B, Hkv, M, k):
+    if scores.shape != (B, Hkv, M) or scores.dtype != torch.float32:
+        raise ValueError("scores must be float32 [B,Hkv,M]")
+    if evict_idx.shape != (B, Hkv, k) or evict_idx.dtype != torch.int32:
+        raise ValueError("evict_idx must be int32 [B,Hkv,T]")
+    if token_pos is not None and (token_pos.dtype != torch.int32 or
+                                  token_pos.shape != (B, Hkv, M)):
+        raise ValueError("token_pos must be int32 [B,Hkv,M]")
+
+
+def h2o_evict_insert_q8(k_codes, k_scales, v_codes, v_scales, scores, token_pos, k_new, v_new,
+                        wsum, evict_idx, pos0: int, policy="h2o", workspace=None,
+                        stream=None) -> None:
+    """h2o_evict_insert_policy over an 8-bit cache; workspace is a uint8 tensor of
+    h2o_evict_workspace_bytes()."""
+    B, Hkv, M, d = _q8_cache(k_codes, k_scales, v_codes, v_scales)
+    T = _q8_rows(k_new, v_new, None, B, Hkv, M, d)
+    _evict_q8(scores, token_pos, evict_idx, B, Hkv, M, T)
+    if wsum.shape != (B, Hkv, M + T) or wsum.dtype != torch.float32:
+        raise ValueError("wsum must be float32 [B,Hkv,M+T]")
+    _check(lib().h2o_evict_insert_q8(
+        *_q8_ptrs(k_codes, k_scales, v_codes, v_scales), _dev(scores, "scores"),
+        _dev(token_pos, "token_pos"), _dev(k_new, "k_new"), _dev(v_new, "v_new"),
+        _dev(wsum, "wsum"), _dev(evict_idx, "evict_idx"), B, Hkv, M, T, d, T, int(pos0),
+        _dtype_code(k_new), _policy_code(policy), _dev(workspace, "workspace"),
+        _nbytes(workspace), _stream(stream)))
+
+
+def h2o_chunk_step_q8(q, k_codes, k_scales, v_codes, v_scales, scores, token_pos, k_new, v_new,
+                      out, lse, wsum, evict_idx, workspace, pos0: int,
+                      scale: Optional[float] = None, policy="h2o", stream=None) -> None:
+    """One chunk step over an 8-bit cache (h2o_sdpa_chunk_q8, h2o_accumulate_scores,
+    h2o_evict_insert_q8); workspace of h2o_q8_workspace_bytes(..., policy) bytes."""
+    sizes = _chunk_q8(q, k_codes, k_scales, v_codes, v_scales, k_new, v_new, out, lse, wsum)
+    B, _, Hkv, T, M, d = sizes
+    _evict_q8(scores, token_pos, evict_idx, B, Hkv, M, T)
+    if scale is None:
+        scale = d ** -0.5
+    _check(lib().h2o_chunk_step_q8(
+        _dev(q, "q"), *_q8_ptrs(k_codes, k_scales, v_codes, v_scales), _dev(scores, "scores"),
+        _dev(token_pos, "token_pos"), _dev(k_new, "k_new"), _dev(v_new, "v_new"),
+        _dev(out, "out"), _dev(lse, "lse"), _dev(wsum, "wsum"), _dev(evict_idx, "evict_idx"),
+        _dev(workspace, "workspace"), _nbytes(workspace), *sizes, float(scale), int(pos0),
+        _dtype_code(q), _policy_code(policy), _stream(stream)))
+
+
+# ----------------------------------------------- a tree of drafted tokens
+def h2o_tree_workspace_bytes(B, Hq, Hkv, T, M, d, dtype) -> int:
+    code = dtype if isinstance(dtype, int) else _dtype_code(torch.empty(0, dtype=dtype))
+    return int(lib().h2o_tree_workspace_bytes(B, Hq, Hkv, T, M, d, code))
+
+
+def _tree_args(q, k_cache, k_scales, k_new, v_new):
+    B, Hq, T, d = q.shape
+    Hkv, M = k_cache.shape[1], k_cache.shape[2]
+    if k_cache.shape != (B, Hkv, M, d):
+        raise ValueError("cache shape mismatch")
+    if k_cache.dtype != (torch.int8 if k_scales is not None else q.dtype):
+        raise TypeError("the cache must be int8 with scales, or in q's dtype without")
+    if k_scales is not None and (k_scales.shape != (B, Hkv, M) or
+                                 k_scales.dtype != torch.float32):
+        raise ValueError("k_scales must be float32 [B,Hkv,M]")
+    for name, t in (("k_new", k_new), ("v_new", v_new)):
+        if t.dtype != q.dtype or t.shape != (B, Hkv, T, d):
+            raise ValueError(f"{name} must be [B,Hkv,T,d] in q's dtype")
+    return B, Hq, Hkv, T, M, d
+
+
+def h2o_sdpa_tree(q, k_cache, v_cache, k_new, v_new, parents, out, lse, workspace,
+                  scale: Optional[float] = None, k_scales=None, v_scales=None,
+                  stream=None) -> None:
+    """Attention of the T nodes of a token tree (parents [B,T] int32, -1 for a root)
+    over the cache, their ancestors and themselves; the cache in q's dtype, or int8
+    codes with k_scales and v_scales [B,Hkv,M] f32."""
+    B, Hq, Hkv, T, M, d = _tree_args(q, k_cache, k_scales, k_new, v_new)
+    if v_cache.shape != k_cache.shape or v_cache.dtype != k_cache.dtype:
+        raise ValueError("v_cache must be like k_cache")
+    if (k_scales is None) != (v_scales is None):
+        raise ValueError("k_scales and v_scales go together")
+    if v_scales is not None and (v_scales.shape != (B, Hkv, M) or
+                                 v_scales.dtype != torch.float32):
+        raise ValueError("v_scales must be float32 [B,Hkv,M]")
+    if parents.dtype != torch.int32 or parents.shape != (B, T):
+        raise ValueError("parents must be int32 [B,T]")
+    if out.shape != (B, Hq, T, d) or out.dtype != q.dtype:
+        raise ValueError("out must be like q")
+    if lse.shape != (B, Hq, T) or lse.dtype != torch.float32:
+        raise ValueError("lse must be float32 [B,Hq,T]")
+    if scale is None:
+        scale = d ** -0.5
+    _check(lib().h2o_sdpa_tree(
+        _dev(q, "q"), _dev(k_cache, "k_cache"), _dev(k_scales, "k_scales"),
+        _dev(v_cache, "v_cache"), _dev(v_scales, "v_scales"), _dev(k_new, "k_new"),
+        _dev(v_new, "v_new"), _dev(parents, "parents"), _dev(out, "out"), _dev(lse, "lse"),
+        _dev(workspace, "workspace"), _nbytes(workspace), B, Hq, Hkv, T, M, d, float(scale),
+        _dtype_code(q), _stream(stream)))
+
+
+def h2o_tree_accept(q, k_cache, k_new, v_new, lse, path, k_acc, v_acc, wsum, workspace,
+                    scale: Optional[float] = None, k_scales=None, stream=None) -> None:
+    """The accepted nodes path [B,A] int32 as a chunk of A tokens: their summed
+    weights wsum [B,Hkv,M+A] f32, keys and values k_acc, v_acc [B,Hkv,A,d], for
+    h2o_accumulate_scores and an h2o_evict_insert call. lse from h2o_sdpa_tree."""
+    B, Hq, Hkv, T, M, d = _tree_args(q, k_cache, k_scales, k_new, v_new)
+    if path.dtype != torch.int32 or path.dim() != 2 or path.shape[0] != B:
+        raise ValueError("path must be int32 [B,A]")
+    A = path.shape[1]
+    for name, t in (("k_acc", k_acc), ("v_acc", v_acc)):
+        if t.dtype != q.dtype or t.shape != (B, Hkv, A, d):
+            raise ValueError(f"{name} must be [B,Hkv,A,d] in q's dtype")
+    if lse.shape != (B, Hq, T) or lse.dtype != torch.float32:
+        raise ValueError("lse must be float32 [B,Hq,T]")
+    if wsum.shape != (B, Hkv, M + A) or wsum.dtype != torch.float32:
+        raise ValueError("wsum must be float32 [B,Hkv,M+A]")
+    if scale is None:
+        scale = d ** -0.5
+    _check(lib().h2o_tree_accept(
+        _dev(q, "q"), _dev(k_cache, "k_cache"), _dev(k_scales, "k_scales"), _dev(k_new, "k_new"),
+        _dev(v_new, "v_new"), _dev(lse, "lse"), _dev(path, "path"), _dev(k_acc, "k_acc"),
+        _dev(v_acc, "v_acc"), _dev(wsum, "wsum"), _dev(workspace, "workspace"),
+        _nbytes(workspace), B, Hq, Hkv, T, M, A, d, float(scale), _dtype_code(q),
+        _stream(stream)))
+
+
 def h2o_bottomk(scores, k: int, idx_out, stream=None) -> None:
     """scores [..., M] f32; idx_out [..., k] int32 (ascending indices)."""
     M = scores.shape[-1]
@@ -499,12 +739,17 @@ def h2o_bottomk(scores, k: int, idx_out, stream=None) -> None:
 
 # ------------------------------------------------------------ conveniences
 def alloc_step(B, Hq, Hkv, T, M, d, dtype, device="cuda", policy="h2o",
-               insert_first: bool = False):
+               insert_first: bool = False, q8: bool = False):
     """Output and scratch tensors for one chunk step (``policy``'s eviction
     workspace included); ``insert_first``: for the paper's order
-    (h2o_chunk_step_insert_first / h2o_sdpa_cache, wsum of M columns)."""
+    (h2o_chunk_step_insert_first / h2o_sdpa_cache, wsum of M columns); ``q8``: for
+    an 8-bit cache (h2o_chunk_step_q8 / h2o_sdpa_chunk_q8)."""
     code = _dtype_code(torch.empty(0, dtype=dtype))
-    if insert_first:
+    if insert_first and q8:
+        raise ValueError("an 8-bit cache has the attend-first order alone")
+    if q8:
+        ws = h2o_q8_workspace_bytes(B, Hq, Hkv, T, M, d, code, policy)
+    elif insert_first:
         ws = h2o_cache_workspace_bytes(B, Hq, Hkv, T, M, d, code, policy)
     else:
         ws = h2o_workspace_bytes(B, Hq, Hkv, T, M, d, code)
@@ -548,3 +793,25 @@ def step(state, q, k_new, v_new, bufs, pos0: int, scale=None, stream=None,
     h2o_accumulate_scores(state["scores"], bufs["wsum"], stream)
     h2o_evict_insert(state["k_cache"], state["v_cache"], state["scores"], state.get("token_pos"),
                      k_new, v_new, bufs["wsum"], bufs["evict_idx"], pos0, stream)
+
+
+def step_q8(state, q, k_new, v_new, bufs, pos0: int, scale=None, stream=None,
+            fused: bool = True, policy: str = "h2o") -> None:
+    """``step`` over an 8-bit cache, through h2o_chunk_step_q8 (``fused``) or its
+    three parts.
+
+    ``state`` holds k_codes, k_scales, v_codes, v_scales, scores, token_pos
+    (token_pos may be None except for h2o_norm); ``bufs`` of alloc_step(..., q8=True).
+    """
+    cache = (state["k_codes"], state["k_scales"], state["v_codes"], state["v_scales"])
+    if fused:
+        h2o_chunk_step_q8(q, *cache, state["scores"], state.get("token_pos"), k_new, v_new,
+                          bufs["out"], bufs["lse"], bufs["wsum"], bufs["evict_idx"],
+                          bufs["workspace"], pos0, scale, policy, stream)
+        return
+    h2o_sdpa_chunk_q8(q, *cache, k_new, v_new, bufs["out"], bufs["lse"], bufs["wsum"],
+                      bufs["workspace"], scale, stream)
+    h2o_accumulate_scores(state["scores"], bufs["wsum"], stream)
+    h2o_evict_insert_q8(*cache, state["scores"], state.get("token_pos"), k_new, v_new,
+                        bufs["wsum"], bufs["evict_idx"], pos0, policy, bufs["evict_workspace"],
+                        stream)

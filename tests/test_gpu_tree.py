@@ -1,0 +1,216 @@
+"""Attention of a drafted token tree and the accepting of a path, against float64."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_2608_19920_amd import h2o as H
+import _gpu as U
+from _q8tree import close, dev, dev_cache, guarded, inputs
+
+pytestmark = pytest.mark.gpu
+
+
+def _parents(kind, B, T, rng):
+    if kind == "chain":
+        return np.tile(np.arange(-1, T - 1), (B, 1)).astype(np.int32)
+    if kind == "star":
+        return np.full((B, T), -1, np.int32)
+    p = np.stack([[int(rng.integers(-1, i)) if i else -1 for i in range(T)] for _ in range(B)])
+    if kind == "odd":          # entries that are no parent count as -1
+        for v in (-9, 2 ** 31 - 1, -2 ** 31):
+            p[int(rng.integers(B)), int(rng.integers(T))] = v
+        p[:, T // 2] = T // 2
+        p[:, T // 3] = T - 1
+    return p.astype(np.int32)
+
+
+TREES = [  # B, Hq, Hkv, d, M, T, parents
+    (1, 1, 1, 64, 1, 1, "star"), (1, 4, 2, 128, 0, 1, "chain"), (2, 4, 2, 64, 0, 33, "random"),
+    (1, 7, 1, 64, 31, 2, "random"), (2, 8, 2, 128, 64, 5, "odd"), (1, 8, 1, 64, 65, 16, "random"),
+    (2, 4, 2, 128, 127, 31, "chain"), (1, 2, 2, 64, 300, 32, "star"), (1, 4, 1, 128, 500, 61, "random"),
+    (2, 2, 1, 64, 63, 64, "odd"), (1, 4, 2, 128, 100, 65, "random"), (1, 2, 1, 64, 90, 130, "random"),
+    (1, 3, 3, 64, 40, 300, "odd"), (1, 16, 1, 128, 2000, 8, "random"), (1, 1, 1, 64, 7, 513, "chain"),
+]
+
+
+def _tree_call(x, case, dtype, q8, parents):
+    B, Hq, Hkv, d, M, T = case[:6]
+    tdt = U.TDT[dtype]
+    out, og = guarded(64, B, Hq, T, d, dtype=tdt)
+    lse, lg = guarded(16, B, Hq, T)
+    n = H.h2o_tree_workspace_bytes(B, Hq, Hkv, T, M, d, tdt)
+    ws, wsg = guarded(64, max(n, 16), dtype=torch.uint8, fill=255)
+    c = dev_cache(x) if q8 else [dev(x["k_cache"], tdt), None, dev(x["v_cache"], tdt), None]
+    U.say("tree", case, dtype, "8-bit" if q8 else "", "workspace", n)
+    H.h2o_sdpa_tree(dev(x["q"], tdt), c[0], c[2], dev(x["k_new"], tdt), dev(x["v_new"], tdt),
+                    dev(parents), out, lse, ws, float(x["scale"]), k_scales=c[1], v_scales=c[3])
+    torch.cuda.synchronize()
+    for g, f in ((og, 7), (lg, 7), (wsg, 255)):
+        assert (g == f).all()
+    return out, lse, ws, c
+
+
+@pytest.mark.parametrize("dtype,q8", [("bf16", False), ("bf16", True), ("f32", False), ("f32", True)])
+@pytest.mark.parametrize("case", TREES, ids=["-".join(map(str, c)) for c in TREES])
+def test_tree(case, dtype, q8):
+    B, Hq, Hkv, d, M, T, kind = case
+    x = inputs(*case[:6], dtype, seed=M + T)
+    parents = _parents(kind, B, T, np.random.default_rng(T))
+    out, lse, _, _ = _tree_call(x, case, dtype, q8, parents)
+    kv = [x[n + ("_values" if q8 else "_cache")] for n in "kv"]
+    o, l = oracle.sdpa_tree(x["q"], *kv, x["k_new"], x["v_new"], parents, x["scale"])
+    close(dtype, str(case), out=(out, o), lse=(lse, l))
+
+
+ACCEPTS = [  # B, Hq, Hkv, d, M, T, A
+    (1, 1, 1, 64, 1, 1, 1), (1, 4, 2, 128, 0, 5, 2), (2, 7, 1, 64, 127, 16, 5),
+    (1, 8, 2, 128, 130, 16, 16), (2, 4, 2, 64, 700, 61, 9), (1, 4, 4, 128, 64, 40, 33),
+    (1, 16, 2, 64, 500, 150, 140), (3, 2, 1, 128, 33, 7, 1),
+]
+
+
+@pytest.mark.parametrize("dtype,q8", [("bf16", False), ("bf16", True), ("f32", False), ("f32", True)])
+@pytest.mark.parametrize("case", ACCEPTS, ids=["-".join(map(str, c)) for c in ACCEPTS])
+def test_accept(case, dtype, q8):
+    B, Hq, Hkv, d, M, T, A = case
+    x, tdt = inputs(*case[:6], dtype, seed=M + T), U.TDT[dtype]
+    rng = np.random.default_rng(A)
+    parents = _parents("random", B, T, rng)
+    path = np.stack([np.sort(rng.permutation(T)[:A]) for _ in range(B)]).astype(np.int32)
+    for b in range(B):
+        parents[b, path[b]] = np.concatenate([[-1], path[b][:-1]])
+    _, lse, ws, c = _tree_call(x, case, dtype, q8, parents)
+    if A > 3:                                   # entries that stand for no token
+        path[0, 1], path[-1, A - 1] = -1, T
+    q, kn, vn = dev(x["q"], tdt), dev(x["k_new"], tdt), dev(x["v_new"], tdt)
+    ka, kg = guarded(64, B, Hkv, A, d, dtype=tdt)
+    va, vg = guarded(64, B, Hkv, A, d, dtype=tdt)
+    wsum, wg = guarded(16, B, Hkv, M + A)
+    ws.fill_(255)
+    U.say("accept", case, dtype, q8)
+    H.h2o_tree_accept(q, c[0], kn, vn, lse, dev(path), ka, va, wsum, ws, float(x["scale"]),
+                      k_scales=c[1])
+    torch.cuda.synchronize()
+    for g in (kg, vg, wg):
+        assert (g == 7).all()
+    w, k, v = oracle.tree_accept(x["q"], x["k_values" if q8 else "k_cache"], x["k_new"], x["v_new"],
+                                 U.to_np(lse), path, x["scale"])
+    np.testing.assert_array_equal(U.to_np(ka), k)
+    np.testing.assert_array_equal(U.to_np(va), v)
+    close(dtype, str(case), wsum=(wsum, w))
+
+
+def test_f32_hidden_nodes_stay_out():
+    """Inf and NaN in a node's key and value reach its descendants and itself alone."""
+    case = (1, 4, 2, 64, 50, 40, "random")
+    x = inputs(*case[:6], "f32", seed=4)
+    parents = _parents("random", 1, 40, np.random.default_rng(2))
+    sees = oracle.ancestors(parents)[0]
+    o, l = oracle.sdpa_tree(x["q"], x["k_cache"], x["v_cache"], x["k_new"], x["v_new"], parents,
+                            x["scale"])
+    x["v_new"][0, 1, 9, 3], x["k_new"][0, 1, 17, 5] = np.inf, np.nan
+    out, lse, ws, c = _tree_call(x, case, "f32", False, parents)
+    clean = ~sees[:, 9] & ~sees[:, 17]
+    assert 5 < clean.sum() < 39
+    close("f32", "hidden", out=(out[:, :, clean], o[:, :, clean]), lse=(lse[:, :, clean], l[:, :, clean]))
+    assert torch.isnan(out[0, 2:, sees[:, 17]]).all()
+    inf = sees[:, 9] & ~sees[:, 17]
+    assert torch.isinf(out[0, 2:, inf, 3]).all() and torch.isfinite(out[0, 2:, inf, 4:]).all()
+    # the columns of nodes on the path: the node of the Inf value is one of them, its
+    # weights are finite
+    path = np.array([[9]], np.int32) if parents[0, 9] == -1 else np.array([[int(np.argmax(clean))]], np.int32)
+    ka, va = (torch.empty(1, 2, 1, 64, device=U.DEV) for _ in range(2))
+    wsum = torch.empty(1, 2, 51, device=U.DEV)
+    H.h2o_tree_accept(dev(x["q"]), c[0], dev(x["k_new"]), dev(x["v_new"]), lse, dev(path), ka, va,
+                      wsum, ws, float(x["scale"]))
+    assert torch.isfinite(wsum).all()
+
+
+@pytest.mark.parametrize("dtype,q8", [("bf16", True), ("f32", False)])
+def test_a_draft_is_the_chunk_of_its_accepted_tokens(dtype, q8):
+    """Draft, attend, accept, evict and insert, several times in a row: the cache and
+    the scores end as after chunk steps of the accepted tokens alone."""
+    B, Hq, Hkv, d, M, T, A = 2, 8, 2, 64, 200, 12, 3
+    x, tdt = inputs(B, Hq, Hkv, d, M, T, dtype, seed=6), U.TDT[dtype]
+    cache = dev_cache(x) if q8 else [dev(x["k_cache"], tdt), None, dev(x["v_cache"], tdt), None]
+    scores, tp = dev(x["scores"]), dev(x["token_pos"])
+    ws = torch.empty(H.h2o_tree_workspace_bytes(B, Hq, Hkv, T, M, d, tdt), dtype=torch.uint8,
+                     device=U.DEV)
+    new = lambda *s, dt=torch.float32: torch.empty(*s, dtype=dt, device=U.DEV)
+    out, lse, wsum = new(B, Hq, T, d, dt=tdt), new(B, Hq, T), new(B, Hkv, M + A)
+    ka, va, idx = new(B, Hkv, A, d, dt=tdt), new(B, Hkv, A, d, dt=tdt), new(B, Hkv, A, dt=torch.int32)
+    rng = np.random.default_rng(0)
+    pos0 = int(x["pos0"])
+    for n in range(3):
+        q, kn, vn = (dev(rng.standard_normal(s).astype(np.float32), tdt)
+                     for s in ((B, Hq, T, d), (B, Hkv, T, d), (B, Hkv, T, d)))
+        parents = _parents("random", B, T, rng)
+        path = np.stack([np.sort(rng.permutation(T)[:A]) for _ in range(B)]).astype(np.int32)
+        for b in range(B):
+            parents[b, path[b]] = np.concatenate([[-1], path[b][:-1]])
+        before = [t.clone() if t is not None else None for t in (*cache, scores, tp)]
+        U.say("draft", n, dtype, q8)
+        H.h2o_sdpa_tree(q, cache[0], cache[2], kn, vn, dev(parents), out, lse, ws,
+                        k_scales=cache[1], v_scales=cache[3])
+        H.h2o_tree_accept(q, cache[0], kn, vn, lse, dev(path), ka, va, wsum, ws, k_scales=cache[1])
+        H.h2o_accumulate_scores(scores, wsum)
+        if q8:
+            H.h2o_evict_insert_q8(*cache, scores, tp, ka, va, wsum, idx, pos0)
+        else:
+            H.h2o_evict_insert(cache[0], cache[2], scores, tp, ka, va, wsum, idx, pos0)
+        torch.cuda.synchronize()
+        # the chunk of the accepted tokens on the state before
+        kv = [U.to_np(before[i]) if not q8 else
+              oracle.dequantize(before[i].cpu().numpy(), before[i + 1].cpu().numpy()) for i in (0, 2)]
+        at = path[:, None, :, None]
+        pick = lambda t: np.take_along_axis(U.to_np(t), np.broadcast_to(at, (B, t.shape[1], A, d)), 2)
+        o, l, w = oracle.sdpa_chunk(pick(q), *kv, pick(kn), pick(vn))
+        close(dtype, f"draft {n}", out=(torch.from_numpy(pick(out)), o), wsum=(wsum, w),
+              lse=(torch.from_numpy(np.take_along_axis(U.to_np(lse), np.broadcast_to(
+                  path[:, None], (B, Hq, A)), 2)), l))
+        # the selection is the oracle's on the summed weights that came out
+        acc = oracle.accumulate_scores(before[4].cpu().numpy(), wsum.cpu().numpy())
+        want = oracle.bottomk(acc, A)
+        assert np.array_equal(idx.cpu().numpy(), want)
+        pos = before[5].cpu().numpy()
+        np.put_along_axis(pos, want.astype(np.int64), np.arange(pos0, pos0 + A, dtype=np.int32)[None, None], 2)
+        assert np.array_equal(tp.cpu().numpy(), pos)
+        pos0 += A
+
+
+def test_captured_drafts_between_eager_ones():
+    """Tree and accept in a graph with new parents and paths at every replay."""
+    B, Hq, Hkv, d, M, T, A = 1, 8, 2, 64, 333, 20, 4
+    x, tdt = inputs(B, Hq, Hkv, d, M, T, "bf16", seed=6), torch.bfloat16
+    c = dev_cache(x)
+    q, kn, vn = dev(x["q"], tdt), dev(x["k_new"], tdt), dev(x["v_new"], tdt)
+    rng = np.random.default_rng(5)
+    par, path = dev(_parents("random", B, T, rng)), dev(np.arange(A, dtype=np.int32)[None])
+
+    def bufs():
+        n = H.h2o_tree_workspace_bytes(B, Hq, Hkv, T, M, d, tdt)
+        new = lambda *s, dt=torch.float32: torch.zeros(*s, dtype=dt, device=U.DEV)
+        return dict(ws=new(n, dt=torch.uint8), out=new(B, Hq, T, d, dt=tdt), lse=new(B, Hq, T),
+                    ka=new(B, Hkv, A, d, dt=tdt), va=new(B, Hkv, A, d, dt=tdt), wsum=new(B, Hkv, M + A))
+
+    def call(b):
+        H.h2o_sdpa_tree(q, c[0], c[2], kn, vn, par, b["out"], b["lse"], b["ws"], k_scales=c[1],
+                        v_scales=c[3])
+        H.h2o_tree_accept(q, c[0], kn, vn, b["lse"], path, b["ka"], b["va"], b["wsum"], b["ws"],
+                          k_scales=c[1])
+
+    one, two = bufs(), bufs()
+    call(one)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=torch.cuda.Stream()):
+        call(one)
+    for n in range(4):
+        par.copy_(dev(_parents("random", B, T, rng)))
+        path.copy_(dev(np.sort(rng.permutation(T)[:A])[None].astype(np.int32)))
+        g.replay()
+        call(two)
+        torch.cuda.synchronize()
+        for k in ("out", "lse", "ka", "va", "wsum"):
+            assert torch.equal(one[k], two[k]), (n, k)
