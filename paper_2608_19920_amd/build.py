@@ -35,7 +35,7 @@ FILE_FLAGS = {
     "decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "sdpa_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"],
     "f32_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-    "flash.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "flash.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"],
     "flash_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "backward_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }

@@ -21,15 +21,20 @@
 #include "mfma_ops.h"
 #include "q8.h"
 
+#include <cmath>
+
 namespace h2o {
 namespace {
 
 using namespace mfma;
 
-constexpr int BN = 64;          // keys per tile
+constexpr int BN = 32;          // keys per tile
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kXcds = 8;
+constexpr int kFewSplits = 4;   // key ranges that one thread merges alone
+// A lambda over register arrays: a call that is not inlined would put them in memory.
+#define H2O_INLINE __attribute__((always_inline))
 
 __host__ __device__ constexpr int lds_pitch(int D) { return D + 16; }   // bf16 per LDS row
 
@@ -46,58 +51,65 @@ struct Args {
 // Blocks reach the 8 XCDs round-robin: the row tiles of one (head, key range),
 // which read the same keys, go to one XCD and share its L2, last rows first.
 struct BlockId { int rt, sp, bh; };
-__device__ __forceinline__ BlockId block_id(int nsplit) {
-  const int nrt = gridDim.x / nsplit, ngroups = nsplit * gridDim.y;
-  const int lin = blockIdx.x + blockIdx.y * gridDim.x;
-  int grp = lin / nrt, i = lin % nrt;
+__device__ __forceinline__ void xcd_group(int lin, int per, int ngroups, int& grp, int& i) {
+  grp = lin / per;
+  i = lin % per;
   if (ngroups % kXcds == 0) {
     const int n = lin / kXcds;
-    grp = (n / nrt) * kXcds + lin % kXcds;
-    i = n % nrt;
+    grp = (n / per) * kXcds + lin % kXcds;
+    i = n % per;
   }
+}
+__device__ __forceinline__ BlockId block_id(int nsplit) {
+  const int nrt = gridDim.x / nsplit;
+  int grp, i;
+  xcd_group(blockIdx.x + blockIdx.y * gridDim.x, nrt, nsplit * gridDim.y, grp, i);
   return BlockId{nrt - 1 - i, grp % nsplit, grp / nsplit};
 }
 
 // ------------------------------------------------------------------- staging
-// A tile's rows in registers: 16-byte units, 16 codes or 8 bf16 each.
-template <int D>
+// A tile's rows in registers: 16-byte units, 16 codes or 8 bf16 each, unit u of
+// thread t being t + u * NT.
+template <int D, int NT>
 struct Regs {
-  static constexpr int N16 = BN * D / 8 / kThreads;
+  static constexpr int N16 = BN * D / 8 / NT;
+  static constexpr int N8 = (BN * D / 16 + NT - 1) / NT;   // (8 waves, D = 64: half the threads)
   u32x4 k[N16], v[N16];
   float s;                      // thread t < BN: scale of key t; BN <= t < 2 BN: of value t - BN
 };
 
-template <int D>
-__device__ __forceinline__ void load_rows16(u32x4 (&r)[Regs<D>::N16], const void* base, int n) {
+template <int D, int NT>
+__device__ __forceinline__ void load_rows16(u32x4* r, const void* base, int n) {
   const char* p = reinterpret_cast<const char*>(base);
 #pragma unroll
-  for (int e = 0; e < Regs<D>::N16; ++e) {
-    const int u = threadIdx.x + e * kThreads, row = min(u / (D / 8), n - 1);
+  for (int e = 0; e < Regs<D, NT>::N16; ++e) {
+    const int u = threadIdx.x + e * NT, row = min(u / (D / 8), n - 1);
     r[e] = *reinterpret_cast<const u32x4*>(p + (uint32_t)(row * D + 8 * (u % (D / 8))) * 2u);
   }
 }
-template <int D>
-__device__ __forceinline__ void load_rows8(u32x4 (&r)[Regs<D>::N16], const void* base, int n) {
+template <int D, int NT>
+__device__ __forceinline__ void load_rows8(u32x4* r, const void* base, int n) {
   const char* p = reinterpret_cast<const char*>(base);
 #pragma unroll
-  for (int e = 0; e < Regs<D>::N16 / 2; ++e) {
-    const int u = threadIdx.x + e * kThreads, row = min(u / (D / 16), n - 1);
+  for (int e = 0; e < Regs<D, NT>::N8; ++e) {
+    const int u = threadIdx.x + e * NT, row = min(u / (D / 16), n - 1);
     r[e] = *reinterpret_cast<const u32x4*>(p + (uint32_t)(row * D + 16 * (u % (D / 16))));
   }
 }
-template <int D>
-__device__ __forceinline__ void store_rows16(bf16_t* lds, const u32x4 (&r)[Regs<D>::N16]) {
+template <int D, int NT>
+__device__ __forceinline__ void store_rows16(bf16_t* lds, const u32x4* r) {
 #pragma unroll
-  for (int e = 0; e < Regs<D>::N16; ++e) {
-    const int u = threadIdx.x + e * kThreads;
+  for (int e = 0; e < Regs<D, NT>::N16; ++e) {
+    const int u = threadIdx.x + e * NT;
     *reinterpret_cast<u32x4*>(lds + u / (D / 8) * lds_pitch(D) + 8 * (u % (D / 8))) = r[e];
   }
 }
-template <int D>
-__device__ __forceinline__ void store_rows8(bf16_t* lds, const u32x4 (&r)[Regs<D>::N16]) {
+template <int D, int NT>
+__device__ __forceinline__ void store_rows8(bf16_t* lds, const u32x4* r) {
 #pragma unroll
-  for (int e = 0; e < Regs<D>::N16 / 2; ++e) {
-    const int u = threadIdx.x + e * kThreads;
+  for (int e = 0; e < Regs<D, NT>::N8; ++e) {
+    const int u = threadIdx.x + e * NT;
+    if (BN * D / 16 < NT && u >= BN * D / 16) return;
     bf16x8* dst = reinterpret_cast<bf16x8*>(lds + u / (D / 16) * lds_pitch(D) + 16 * (u % (D / 16)));
     dst[0] = q8::codes_bf16(r[e][0], r[e][1]);
     dst[1] = q8::codes_bf16(r[e][2], r[e][3]);
@@ -105,52 +117,67 @@ __device__ __forceinline__ void store_rows8(bf16_t* lds, const u32x4 (&r)[Regs<D
 }
 
 // Rows past the tile's end re-read its last row (in bounds; masked later).
-template <int D, bool Q8>
-__device__ __forceinline__ void load_tile(Regs<D>& g, const Args& a, size_t bh, int t, int tc) {
-  if (t < tc) {
-    const int j0 = t * BN, n = min(BN, a.M - j0);
+// WHOLE: the caller knows that it is a whole cache tile (no branch).
+template <int D, bool Q8, int NT, bool WHOLE = false>
+__device__ __forceinline__ void load_tile(Regs<D, NT>& g, const Args& a, size_t bh, int t, int tc) {
+  if (WHOLE || t < tc) {
+    const int j0 = t * BN, n = WHOLE ? BN : min(BN, a.M - j0);
     const size_t row = bh * (size_t)a.M + j0;
     if constexpr (Q8) {
-      load_rows8<D>(g.k, (const int8_t*)a.kc + row * D, n);
-      load_rows8<D>(g.v, (const int8_t*)a.vc + row * D, n);
+      load_rows8<D, NT>(g.k, (const int8_t*)a.kc + row * D, n);
+      load_rows8<D, NT>(g.v, (const int8_t*)a.vc + row * D, n);
       const int r = threadIdx.x % BN;
       if (threadIdx.x < 2 * BN) g.s = (threadIdx.x < BN ? a.ks : a.vs)[row + min(r, n - 1)];
     } else {
-      load_rows16<D>(g.k, (const bf16_t*)a.kc + row * D, n);
-      load_rows16<D>(g.v, (const bf16_t*)a.vc + row * D, n);
+      load_rows16<D, NT>(g.k, (const bf16_t*)a.kc + row * D, n);
+      load_rows16<D, NT>(g.v, (const bf16_t*)a.vc + row * D, n);
     }
   } else {
     const int j0 = (t - tc) * BN, n = min(BN, a.T - j0);
     const size_t row = bh * (size_t)a.T + j0;
-    load_rows16<D>(g.k, a.kn + row * D, n);
-    load_rows16<D>(g.v, a.vn + row * D, n);
+    load_rows16<D, NT>(g.k, a.kn + row * D, n);
+    load_rows16<D, NT>(g.v, a.vn + row * D, n);
     if (Q8) g.s = 1.f;
   }
 }
-template <int D, bool Q8>
-__device__ __forceinline__ void store_tile(bf16_t* Ks, bf16_t* Vs, float* sc, const Regs<D>& g,
-                                           const Args& a, int t, int tc) {
-  if (Q8 && t < tc) {
-    store_rows8<D>(Ks, g.k);
-    store_rows8<D>(Vs, g.v);
+template <int D, bool Q8, int NT, bool WHOLE = false>
+__device__ __forceinline__ void store_tile(bf16_t* Ks, bf16_t* Vs, float* sc,
+                                           const Regs<D, NT>& g, const Args& a, int t, int tc) {
+  if (Q8 && (WHOLE || t < tc)) {
+    store_rows8<D, NT>(Ks, g.k);
+    store_rows8<D, NT>(Vs, g.v);
   } else {
-    store_rows16<D>(Ks, g.k);
-    store_rows16<D>(Vs, g.v);
+    store_rows16<D, NT>(Ks, g.k);
+    store_rows16<D, NT>(Vs, g.v);
   }
   if (Q8 && threadIdx.x < 2 * BN) sc[threadIdx.x] = threadIdx.x < BN ? g.s * a.c : g.s;
 }
 
 // --------------------------------------------------------------------- flash
-// Each wave owns 16 NQB consecutive packed rows r = i*G + g. The reference
-// maximum mu of a row (log2 units, common to the 4 lanes that hold it) is raised
-// only when a score exceeds it by more than 64, a wave-uniform and rare branch:
-// terms stay below 2^64, far inside float32 and bf16.
-template <int D, bool Q8, bool TREE, int NQB>
-__global__ __launch_bounds__(kThreads) void flash_pass(Args a, int nsplit, bf16_t* __restrict__ out,
-                                                       float* __restrict__ lse,
-                                                       float2* __restrict__ stats,
-                                                       float* __restrict__ opart) {
-  constexpr int ROWS = kWaves * NQB * 16, P = lds_pitch(D), NK = BN / 16;
+// Each of NW waves owns 16 NQB consecutive packed rows r = i*G + g. A row's
+// probabilities are exp2(x - mu) with x its scores in log2 units and mu a
+// reference common to the 4 lanes that hold the row: the maximum of the first
+// tile the row sees, raised when a score exceeds it by more than 64 (a
+// wave-uniform and rare branch), so terms stay below 2^64, far inside float32 and
+// bf16.
+//
+// Tile t + 2 is on its way from memory to registers and tile t + 1 from registers to
+// the other LDS buffer while tile t is used; one barrier a tile. (Multiplying the
+// scores of tile t + 1 during the exponentials of tile t, a third buffer, requests
+// another tile ahead, or an imposed order of products and vector operations, measured
+// no faster: B1 Hq32 Hkv8 d128 M8192 T1024 216 us in every form, 4 waves a block.)
+//
+// Bound by the two pipes of a SIMD together: 32 products (16 cycles each) and some 190
+// vector operations, 16 of them exponentials (8 cycles), per 32 keys and 32 rows; 64
+// of the 190 turn codes into bf16. With 8 waves a block they are half as many per row:
+// 191 us at the shape above, 765 TFLOP/s on the visible pairs.
+template <int D, bool Q8, bool TREE, int NQB, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
+                                                         bf16_t* __restrict__ out,
+                                                         float* __restrict__ lse,
+                                                         float2* __restrict__ stats,
+                                                         float* __restrict__ opart) {
+  constexpr int NT = NW * 64, ROWS = NW * NQB * 16, P = lds_pitch(D);
   __shared__ __attribute__((aligned(16))) bf16_t Ks[2][BN * P];
   __shared__ __attribute__((aligned(16))) bf16_t Vs[2][BN * P];
   __shared__ __attribute__((aligned(16))) float sc[2][2 * BN];
@@ -171,7 +198,7 @@ __global__ __launch_bounds__(kThreads) void flash_pass(Args a, int nsplit, bf16_
 
   bf16x8 qf[NQB][D / 32];
   int qi[NQB];
-  float m[NQB], mu[NQB], l[NQB];
+  float mu[NQB], thr[NQB], l[NQB];
   f32x4 oacc[D / 16][NQB];
 #pragma unroll
   for (int n = 0; n < NQB; ++n) {
@@ -182,123 +209,122 @@ __global__ __launch_bounds__(kThreads) void flash_pass(Args a, int nsplit, bf16_
     qi[n] = i;
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) qf[n][s] = *reinterpret_cast<const bf16x8*>(src + 32 * s);
-    m[n] = -INFINITY;
     mu[n] = 0.f;
+    thr[n] = -INFINITY;               // no tile seen yet
     l[n] = 0.f;
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) oacc[db][n] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  auto tile = [&](auto masked, int t, int buf) {
-    constexpr bool MASK = decltype(masked)::value;
-    f32x4 s[NK][NQB];
+  // Tile t, in LDS at K, V, scl: scores, probabilities, O += P V; then the registers g,
+  // with tile t + 1, go to the other buffer, and tile t + 2 is requested into them.
+  auto tile = [&](auto masked, auto whole, int t, const bf16_t* K, const bf16_t* V,
+                  const float* scl, Regs<D, NT>& g, int t1st, int t2nd, bf16_t* K2, bf16_t* V2,
+                  float* scl2) H2O_INLINE {
+    constexpr bool MASK = decltype(masked)::value, WHOLE = decltype(whole)::value;
+    f32x4 s[2][NQB];
 #pragma unroll
-    for (int kb = 0; kb < NK; ++kb) {
+    for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
       for (int n = 0; n < NQB; ++n) s[kb][n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) {
-        const bf16x8 kf = row_operand(Ks[buf], P, 16 * kb + l16, 32 * x, lane);
+        const bf16x8 kf = row_operand(K, P, 16 * kb + l16, 32 * x, lane);
 #pragma unroll
         for (int n = 0; n < NQB; ++n) s[kb][n] = mma(kf, qf[n][x], s[kb][n]);
       }
     }
     const bool cache = t < tc;
-    uint32_t seen[NQB][BN / 32];
-    if (MASK && TREE && !cache) {
+    uint32_t seen[NQB];
+    if (MASK && TREE && !cache)
 #pragma unroll
-      for (int n = 0; n < NQB; ++n)
+      for (int n = 0; n < NQB; ++n) seen[n] = a.bits[((size_t)b * a.T + qi[n]) * a.W + (t - tc)];
+    f32x4 cks[2], cvs[2];
+    if (Q8)
 #pragma unroll
-        for (int w = 0; w < BN / 32; ++w) {
-          const int word = (t - tc) * (BN / 32) + w;
-          seen[n][w] = word < a.W ? a.bits[((size_t)b * a.T + qi[n]) * a.W + word] : 0u;
-        }
-    }
-    float mx[NQB];
+      for (int kb = 0; kb < 2; ++kb) {
+        cks[kb] = *reinterpret_cast<const f32x4*>(scl + 16 * kb + 4 * g4);
+        cvs[kb] = *reinterpret_cast<const f32x4*>(scl + BN + 16 * kb + 4 * g4);
+      }
+    auto shifted = [&](int n, float ref, float (&x)[8]) H2O_INLINE {
 #pragma unroll
-    for (int n = 0; n < NQB; ++n) mx[n] = -INFINITY;
-#pragma unroll
-    for (int kb = 0; kb < NK; ++kb) {
-      f32x4 cks;
-      if (Q8) cks = *reinterpret_cast<const f32x4*>(&sc[buf][16 * kb + 4 * g4]);
-#pragma unroll
-      for (int n = 0; n < NQB; ++n)
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          float x = s[kb][n][r] * (Q8 ? cks[r] : a.c);
+          float v = fmaf(s[kb][n][r], Q8 ? cks[kb][r] : a.c, -ref);
           if (MASK) {
             const int j = 16 * kb + 4 * g4 + r;
             const bool hid = cache ? t * BN + j >= a.M
-                             : TREE ? !((seen[n][kb >> 1] >> (j & 31)) & 1u)
-                                    : (t - tc) * BN + j > qi[n];
-            if (hid) x = -INFINITY;
+                             : TREE ? !((seen[n] >> j) & 1u) : (t - tc) * BN + j > qi[n];
+            if (hid) v = -INFINITY;
           }
-          s[kb][n][r] = x;
-          mx[n] = fmaxf(mx[n], x);
+          x[4 * kb + r] = v;
         }
-    }
+    };
+    float x[NQB][8], mx[NQB];
     bool up = false;
 #pragma unroll
-    for (int n = 0; n < NQB; ++n) up |= mx[n] > m[n] + 64.f;
+    for (int n = 0; n < NQB; ++n) {
+      shifted(n, mu[n], x[n]);
+      mx[n] = fmaxf(fmaxf(fmaxf(x[n][0], x[n][1]), x[n][2]),
+                    fmaxf(fmaxf(fmaxf(x[n][3], x[n][4]), x[n][5]), fmaxf(x[n][6], x[n][7])));
+      up |= mx[n] > thr[n];
+    }
     if (__builtin_amdgcn_ballot_w64(up)) {
 #pragma unroll
       for (int n = 0; n < NQB; ++n) {
-        float x = fmaxf(mx[n], __shfl_xor(mx[n], 16, 64));
-        x = fmaxf(x, __shfl_xor(x, 32, 64));
-        const bool raise = x > m[n] + 64.f;
-        const float f = raise ? __builtin_amdgcn_exp2f(m[n] - x) : 1.f;
+        float y = fmaxf(mx[n], __shfl_xor(mx[n], 16, 64));
+        y = fmaxf(y, __shfl_xor(y, 32, 64));
+        const bool raise = y > thr[n];
+        const float f = !raise ? 1.f : thr[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(-y);
         l[n] *= f;
 #pragma unroll
         for (int db = 0; db < D / 16; ++db) oacc[db][n] *= f;
-        m[n] = raise ? x : m[n];
-        mu[n] = raise ? x : mu[n];
+        mu[n] = raise ? mu[n] + y : mu[n];
+        thr[n] = raise ? 64.f : thr[n];
+        shifted(n, mu[n], x[n]);
       }
     }
+    bf16x8 pb[NQB];
 #pragma unroll
-    for (int kk = 0; kk < BN / 32; ++kk) {
-      f32x4 sv[2];
-      if (Q8)
+    for (int n = 0; n < NQB; ++n)
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-          sv[u] = *reinterpret_cast<const f32x4*>(&sc[buf][BN + 32 * kk + 16 * u + 4 * g4]);
-      bf16x8 pb[NQB];
-#pragma unroll
-      for (int n = 0; n < NQB; ++n)
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float p = __builtin_amdgcn_exp2f(s[2 * kk + u][n][r] - mu[n]);
-            l[n] += p;
-            pb[n][4 * u + r] = (__bf16)(Q8 ? p * sv[u][r] : p);
-          }
-#pragma unroll
-      for (int db = 0; db < D / 16; ++db) {
-        const bf16x8 vf = tr_operand(Vs[buf] + 32 * kk * P, P, db, lane);
-#pragma unroll
-        for (int n = 0; n < NQB; ++n) oacc[db][n] = mma(vf, pb[n], oacc[db][n]);
+      for (int e = 0; e < 8; ++e) {
+        const float p = __builtin_amdgcn_exp2f(x[n][e]);
+        l[n] += p;
+        pb[n][e] = (__bf16)(Q8 ? p * cvs[e >> 2][e & 3] : p);
       }
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) {
+      const bf16x8 vf = tr_operand(V, P, db, lane);
+#pragma unroll
+      for (int n = 0; n < NQB; ++n) oacc[db][n] = mma(vf, pb[n], oacc[db][n]);
     }
+    store_tile<D, Q8, NT, WHOLE>(K2, V2, scl2, g, a, t1st, tc);
+    load_tile<D, Q8, NT, WHOLE>(g, a, bh, t2nd, tc);
+    __syncthreads();
   };
 
-  // two LDS buffers, one barrier a tile: while tile t is used, tile t + 1 goes
-  // from registers to the other buffer and the loads of tile t + 2 are in flight
   if (t0 < t1) {
-    Regs<D> g;
-    load_tile<D, Q8>(g, a, bh, t0, tc);
-    store_tile<D, Q8>(Ks[0], Vs[0], sc[0], g, a, t0, tc);
-    if (t0 + 1 < t1) load_tile<D, Q8>(g, a, bh, t0 + 1, tc);
+    Regs<D, NT> g;
+    const int last = t1 - 1;
+    load_tile<D, Q8, NT>(g, a, bh, t0, tc);
+    store_tile<D, Q8, NT>(Ks[0], Vs[0], sc[0], g, a, t0, tc);
+    load_tile<D, Q8, NT>(g, a, bh, min(t0 + 1, last), tc);
     __syncthreads();
-    for (int t = t0; t < t1; ++t) {
-      const int buf = (t - t0) & 1;
-      if (t + 1 < t1) {
-        store_tile<D, Q8>(Ks[buf ^ 1], Vs[buf ^ 1], sc[buf ^ 1], g, a, t + 1, tc);
-        if (t + 2 < t1) load_tile<D, Q8>(g, a, bh, t + 2, tc);
+    auto run = [&](auto masked, auto whole, int ta, int tb) H2O_INLINE {
+      for (int t = ta; t < tb; ++t) {
+        const int v = (t - t0) & 1;
+        tile(masked, whole, t, Ks[v], Vs[v], sc[v], g, min(t + 1, last), min(t + 2, last),
+             Ks[v ^ 1], Vs[v ^ 1], sc[v ^ 1]);   // (past the last tile: it again, not used)
       }
-      if (t < tm) tile(IntConst<0>{}, t, buf);
-      else tile(IntConst<1>{}, t, buf);
-      __syncthreads();
-    }
+    };
+    // turns whose tiles t + 1 and t + 2 are whole cache tiles; the others without a
+    // mask; those that ask for it
+    const int te = max(t0, min(t1, tm)), tw = max(t0, min(te, min(t1, tm) - 2));
+    run(IntConst<0>{}, IntConst<1>{}, t0, tw);
+    run(IntConst<0>{}, IntConst<0>{}, tw, te);
+    run(IntConst<1>{}, IntConst<0>{}, te, t1);
   }
 
   const int BH = gridDim.y;
@@ -312,8 +338,8 @@ __global__ __launch_bounds__(kThreads) void flash_pass(Args a, int nsplit, bf16_
     const size_t orow = (size_t)(b * a.Hq + h * a.G + gg) * a.T + qi[n];
     const size_t prow = ((size_t)id.sp * BH + bh) * a.R + r;
     if (g4 == 0) {
-      if (nsplit == 1) lse[orow] = (m[n] + __log2f(L)) * kLn2;
-      else stats[prow] = make_float2(m[n], L);
+      if (nsplit == 1) lse[orow] = (mu[n] + __log2f(L)) * kLn2;
+      else stats[prow] = make_float2(thr[n] == -INFINITY ? -INFINITY : mu[n], L);
     }
     const float inv = 1.f / L;
 #pragma unroll
@@ -321,10 +347,10 @@ __global__ __launch_bounds__(kThreads) void flash_pass(Args a, int nsplit, bf16_
       const f32x4 o = oacc[db][n];
       if (nsplit == 1) {
         typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-        bf16x4 v;
+        bf16x4 w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (__bf16)(o[e] * inv);
-        *reinterpret_cast<bf16x4*>(out + orow * D + 16 * db + 4 * g4) = v;
+        for (int e = 0; e < 4; ++e) w[e] = (__bf16)(o[e] * inv);
+        *reinterpret_cast<bf16x4*>(out + orow * D + 16 * db + 4 * g4) = w;
       } else {
         *reinterpret_cast<f32x4*>(opart + prow * D + 16 * db + 4 * g4) = o;
       }
@@ -332,30 +358,68 @@ __global__ __launch_bounds__(kThreads) void flash_pass(Args a, int nsplit, bf16_
   }
 }
 
-// One packed row per D / 4 threads: the ranges' partials in their order.
-template <int D, typename E>
+// The ranges' partials of a packed row, in a fixed order: D / 4 threads with 4
+// columns each and, with SG > 1, SG such groups that take every SG-th range and
+// meet in LDS. Few ranges come with many rows (SG = 1); many ranges with few,
+// where what counts is that a thread's loads are all in flight at once.
+template <int D, typename E, int SG>
 __global__ __launch_bounds__(kThreads) void flash_combine(const float2* __restrict__ stats,
                                                           const float* __restrict__ opart,
                                                           E* __restrict__ out,
                                                           float* __restrict__ lse, int BH, int Hq,
                                                           int Hkv, int G, int T, int R,
                                                           int nsplit) {
-  constexpr int TPR = D / 4;
-  const size_t row = (size_t)blockIdx.x * (kThreads / TPR) + threadIdx.x / TPR;
-  if (row >= (size_t)BH * R) return;
-  const int c4 = 4 * (threadIdx.x % TPR), bh = (int)(row / R), r = (int)(row % R);
-  const size_t plane = (size_t)BH * R;
+  constexpr int TPR = D / 4, RPB = kThreads / (TPR * SG);   // rows per block
+  constexpr int N = SG > 1 ? kMaxFlashSplit / SG : kFewSplits;
+  static_assert(RPB >= 1 && N * SG >= (SG > 1 ? kMaxFlashSplit : 1), "ranges per thread");
+  __shared__ __attribute__((aligned(16))) f32x4 os[RPB][SG][SG > 1 ? TPR : 1];
+  __shared__ float ls[RPB][SG];
+  const int t = threadIdx.x % TPR, sg = threadIdx.x / TPR % SG, rb = threadIdx.x / (TPR * SG);
+  const size_t rows = (size_t)BH * R, at = (size_t)blockIdx.x * RPB + rb;
+  const size_t row = at < rows ? at : rows - 1;   // (a spare row of threads repeats the last)
+  const int c4 = 4 * t, bh = (int)(row / R), r = (int)(row % R);
+  float2 st[N];
+  f32x4 v[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const int s = k * SG + sg;
+    st[k] = make_float2(-INFINITY, 0.f);
+    v[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (s < nsplit) {
+      st[k] = stats[s * rows + row];
+      v[k] = *reinterpret_cast<const f32x4*>(opart + (s * rows + row) * D + c4);
+    }
+  }
   float mx = -INFINITY;
-  for (int s = 0; s < nsplit; ++s) mx = fmaxf(mx, stats[s * plane + row].x);
+#pragma unroll
+  for (int k = 0; k < N; ++k) mx = fmaxf(mx, st[k].x);
+  if constexpr (SG > 1) {
+    __shared__ float ms[RPB][SG];
+    if (t == 0) ms[rb][sg] = mx;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < SG; ++k) mx = fmaxf(mx, ms[rb][k]);
+  }
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   float L = 0.f;
-  for (int s = 0; s < nsplit; ++s) {
-    const float2 st = stats[s * plane + row];
-    const f32x4 v = *reinterpret_cast<const f32x4*>(opart + (s * plane + row) * D + c4);
-    const float w = st.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.x - mx);
-    L = fmaf(w, st.y, L);
-    o += w * v;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const float w = st[k].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[k].x - mx);
+    L = fmaf(w, st[k].y, L);
+    o += w * v[k];
   }
+  if constexpr (SG > 1) {
+    os[rb][sg][t] = o;
+    if (t == 0) ls[rb][sg] = L;
+    __syncthreads();
+    if (sg) return;
+#pragma unroll
+    for (int k = 1; k < SG; ++k) {
+      o += os[rb][k][t];
+      L += ls[rb][k];
+    }
+  }
+  if (at >= rows) return;
   const int b = bh / Hkv, h = bh % Hkv;
   const size_t orow = (size_t)(b * Hq + h * G + r % G) * T + r / G;
   if (c4 == 0) lse[orow] = (mx + __log2f(L)) * kLn2;
@@ -364,10 +428,10 @@ __global__ __launch_bounds__(kThreads) void flash_combine(const float2* __restri
     *reinterpret_cast<f32x4*>(out + orow * D + c4) = o * inv;
   } else {
     typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    bf16x4 v;
+    bf16x4 w;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (__bf16)(o[e] * inv);
-    *reinterpret_cast<bf16x4*>(out + orow * D + c4) = v;
+    for (int e = 0; e < 4; ++e) w[e] = (__bf16)(o[e] * inv);
+    *reinterpret_cast<bf16x4*>(out + orow * D + c4) = w;
   }
 }
 
@@ -383,18 +447,24 @@ struct ColArgs {
   bf16_t *k_acc, *v_acc;        // path: [BH][A][D], the path's keys and values
   int ncopy;                    // blocks that copy them
 };
-constexpr int kQRows = 32;      // rows per step
+constexpr int kQRows = 64;      // rows per step
 
-template <int D, bool Q8, bool PATH, int NKB>
-__global__ __launch_bounds__(kThreads) void column_pass(Args a, ColArgs p) {
-  constexpr int KB = kWaves * NKB * 16, P = lds_pitch(D), NU = kQRows * D / 8 / kThreads;
+template <int D, bool Q8, bool PATH, int NKB, int NW>
+__global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void column_pass(Args a, ColArgs p) {
+  constexpr int NT = NW * 64, KB = NW * NKB * 16, P = D + 8, NU = kQRows * D / 8 / NT;
   __shared__ __attribute__((aligned(16))) bf16_t Qs[2][kQRows * P];
   __shared__ float lam[2][kQRows];
   __shared__ int pos[2][kQRows];
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const size_t bh = blockIdx.y;
-  const int b = (int)bh / a.Hkv, h = (int)bh % a.Hkv;
+  // a head's blocks, which read the same rows, on one XCD
+  int bhi, bx;
+  xcd_group(blockIdx.x + gridDim.x * (blockIdx.z + gridDim.z * blockIdx.y), gridDim.x * gridDim.z,
+            gridDim.y, bhi, bx);
+  const int bz = bx / gridDim.x;
+  bx %= gridDim.x;
+  const size_t bh = bhi;
+  const int b = bhi / a.Hkv, h = bhi % a.Hkv;
   const int tc = (a.M + KB - 1) / KB, tn = (p.A + KB - 1) / KB;
   const int32_t* path = PATH ? p.path + (size_t)b * p.A : nullptr;
   // node of the chunk's key or row position i, -1 if it is none
@@ -403,9 +473,9 @@ __global__ __launch_bounds__(kThreads) void column_pass(Args a, ColArgs p) {
     const int n = path[i];
     return (unsigned)n < (unsigned)a.T ? n : -1;
   };
-  if (PATH && (int)blockIdx.x >= tc + tn) {   // the path's rows, 16 bytes a thread
-    const int e = ((int)blockIdx.x - tc - tn) * kThreads + tid, i = e / (D / 8), c = e % (D / 8);
-    if (blockIdx.z || i >= p.A) return;
+  if (PATH && bx >= tc + tn) {   // the path's rows, 16 bytes a thread
+    const int e = (bx - tc - tn) * NT + tid, i = e / (D / 8), c = e % (D / 8);
+    if (bz || i >= p.A) return;
     const int n = node_of(i);
     u32x4 kv = {0u, 0u, 0u, 0u}, vv = kv;
     if (n >= 0) {
@@ -416,8 +486,8 @@ __global__ __launch_bounds__(kThreads) void column_pass(Args a, ColArgs p) {
     reinterpret_cast<u32x4*>(p.v_acc + (bh * p.A + i) * (size_t)D)[c] = vv;
     return;
   }
-  const bool cache = (int)blockIdx.x < tc;
-  const int j0 = (cache ? (int)blockIdx.x : (int)blockIdx.x - tc) * KB + wave * NKB * 16;
+  const bool cache = bx < tc;
+  const int j0 = (cache ? bx : bx - tc) * KB + wave * NKB * 16;
   const int nkeys = cache ? a.M : p.A;
   // this lane's operand rows: key j0 + 16 kb + l16, elements 64 x + 16 g4 .. +15
   // (an order of d that both operands share; 16 codes are one load)
@@ -453,74 +523,97 @@ __global__ __launch_bounds__(kThreads) void column_pass(Args a, ColArgs p) {
   }
   // rows of this block: its share of the steps, in a chunk tile from the first
   // row that sees the block's first key
-  const int first = cache ? 0 : ((int)blockIdx.x - tc) * KB * a.G / kQRows;
+  const int first = cache ? 0 : (bx - tc) * KB * a.G / kQRows;
   const int steps = (p.R + kQRows - 1) / kQRows;
   const int per = (steps + (int)gridDim.z - 1) / (int)gridDim.z;
-  const int s1 = min(steps, ((int)blockIdx.z + 1) * per), s0 = max(first, (int)blockIdx.z * per);
+  const int s1 = min(steps, (bz + 1) * per), s0 = max(first, bz * per);
 
+  // A thread's NU units of a step lie NT / (D / 8) rows apart. Its rows, as (position
+  // i, head g of the group), advance by kQRows a step without a division; past the
+  // last row they stay at it (the weights of such rows are 0).
+  constexpr int RU = NT / (D / 8);
   u32x4 qr[NU];
   float lr = 0.f;
-  int ir = 0;
-  auto load = [&](int s) {
+  int ir = 0, ri[NU], rg[NU], li, lg;
+  const int part = 8 * (tid % (D / 8)), di = kQRows / a.G, dg = kQRows % a.G;
+#pragma unroll
+  for (int e = 0; e < NU; ++e) {
+    const int r = s0 * kQRows + tid / (D / 8) + e * RU;
+    ri[e] = r / a.G;
+    rg[e] = r % a.G;
+  }
+  li = (s0 * kQRows + tid) / a.G;
+  lg = (s0 * kQRows + tid) % a.G;
+  const bf16_t* qh = a.q + (size_t)(b * a.Hq + h * a.G) * a.T * D + part;
+  const float* lh = p.lse + (size_t)(b * a.Hq + h * a.G) * a.T;
+  auto advance = [&](int& i, int& g) H2O_INLINE {
+    i += di;
+    g += dg;
+    if (g >= a.G) { g -= a.G; ++i; }
+  };
+  auto load = [&]() H2O_INLINE {   // the rows of the next step
 #pragma unroll
     for (int e = 0; e < NU; ++e) {
-      const int u = tid + e * kThreads, r = min(s * kQRows + u / (D / 8), p.R - 1);
-      const int n = max(node_of(r / a.G), 0);
-      qr[e] = *reinterpret_cast<const u32x4*>(
-          a.q + ((size_t)(b * a.Hq + h * a.G + r % a.G) * a.T + n) * D + 8 * (u % (D / 8)));
+      const int i = min(ri[e], p.A - 1), n = max(node_of(i), 0);
+      qr[e] = *reinterpret_cast<const u32x4*>(qh + (uint32_t)(rg[e] * a.T + n) * (uint32_t)D);
+      advance(ri[e], rg[e]);
     }
     if (tid < kQRows) {   // a row that is none: lambda +inf, weights 0
-      const int r = s * kQRows + tid, n = r < p.R ? node_of(r / a.G) : -1;
-      lr = n >= 0 ? p.lse[(size_t)(b * a.Hq + h * a.G + r % a.G) * a.T + n] * kLog2e : INFINITY;
-      ir = r / a.G;
+      const int n = li < p.A ? node_of(li) : -1;
+      lr = n >= 0 ? lh[lg * a.T + n] * kLog2e : INFINITY;
+      ir = li;
+      advance(li, lg);
     }
   };
-  auto store = [&](int buf) {
+  auto store = [&](int buf) H2O_INLINE {
 #pragma unroll
-    for (int e = 0; e < NU; ++e) {
-      const int u = tid + e * kThreads;
-      *reinterpret_cast<u32x4*>(&Qs[buf][u / (D / 8) * P + 8 * (u % (D / 8))]) = qr[e];
-    }
+    for (int e = 0; e < NU; ++e)
+      *reinterpret_cast<u32x4*>(&Qs[buf][(tid / (D / 8) + e * RU) * P + part]) = qr[e];
     if (tid < kQRows) {
       lam[buf][tid] = lr;
       pos[buf][tid] = ir;
     }
   };
-  auto step = [&](auto chunk, int buf) {
+  // the products of the next 16 rows go out before the exponentials of these
+  auto step = [&](auto chunk, int buf) H2O_INLINE {
+    f32x4 s[2][NKB];
+    auto product = [&](f32x4 (&d)[NKB], int n) H2O_INLINE {
 #pragma unroll
-    for (int n = 0; n < kQRows / 16; ++n) {
-      f32x4 s[NKB];
-#pragma unroll
-      for (int kb = 0; kb < NKB; ++kb) s[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int kb = 0; kb < NKB; ++kb) d[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) {
         const bf16x8 qf = *reinterpret_cast<const bf16x8*>(
             &Qs[buf][(16 * n + l16) * P + 64 * (x >> 1) + 16 * g4 + 8 * (x & 1)]);
 #pragma unroll
-        for (int kb = 0; kb < NKB; ++kb) s[kb] = mma(kf[kb][x], qf, s[kb]);
+        for (int kb = 0; kb < NKB; ++kb) d[kb] = mma(kf[kb][x], qf, d[kb]);
       }
+    };
+    product(s[0], 0);
+#pragma unroll
+    for (int n = 0; n < kQRows / 16; ++n) {
+      if (n + 1 < kQRows / 16) product(s[(n + 1) & 1], n + 1);
       const float la = lam[buf][16 * n + l16];
       const int i = decltype(chunk)::value ? pos[buf][16 * n + l16] : 0;
 #pragma unroll
       for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          float w = __builtin_amdgcn_exp2f(fmaf(s[kb][r], cks[kb][r], -la));
+          float w = __builtin_amdgcn_exp2f(fmaf(s[n & 1][kb][r], cks[kb][r], -la));
           if (decltype(chunk)::value && j0 + 16 * kb + 4 * g4 + r > i) w = 0.f;
           cs[kb][r] += w;
         }
     }
   };
   if (s0 < s1) {
-    load(s0);
+    load();
     store(0);
-    if (s0 + 1 < s1) load(s0 + 1);
+    if (s0 + 1 < s1) load();
     __syncthreads();
     for (int s = s0; s < s1; ++s) {
       const int buf = (s - s0) & 1;
       if (s + 1 < s1) {
         store(buf ^ 1);
-        if (s + 2 < s1) load(s + 2);
+        if (s + 2 < s1) load();
       }
       if (cache) step(IntConst<0>{}, buf);
       else step(IntConst<1>{}, buf);
@@ -528,7 +621,7 @@ __global__ __launch_bounds__(kThreads) void column_pass(Args a, ColArgs p) {
     }
   }
   const int nk = a.M + p.A;
-  float* dst = p.dst + ((size_t)blockIdx.z * gridDim.y + bh) * nk + (cache ? 0 : a.M);
+  float* dst = p.dst + ((size_t)bz * gridDim.y + bh) * nk + (cache ? 0 : a.M);
 #pragma unroll
   for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
@@ -603,22 +696,43 @@ Args make_args(const FlashShape& s, const FlashIn& in, const char* ws, const Fla
 
 }  // namespace
 
-// Rows per block: 128 (32 per wave: every K and V operand read from LDS feeds two
-// products) where there are more than 64. Key ranges: enough blocks for two per
-// CU, at least two tiles each, at most kMaxFlashSplit (each leaves a float32
-// partial of its rows). Row ranges of the column sums: likewise, at least four
-// steps each.
+// Rows per block and key ranges of the flash pass: those of least estimated time.
+// us[k - 1]: microseconds per 32-key tile of a block that shares its CU with k - 1
+// others (8-bit cache, Hkv8 G4 M8192; `resident` is what registers allow); a round takes
+// every block's tiles at full residency, the last one at what is left, and 5 us to
+// start and end; the partials of several ranges are written, read and merged (3 us
+// and a byte of them in 1 / 3 TB/s). At B1 Hkv8 G4 T1024 d128 the plan takes 256 rows
+// and two ranges, 193 + 8 us; 128 rows 221 + 8, four ranges 206 + 13. At d64 256 rows
+// and two ranges 140 + 5, 128 rows and three 145 + 6. At T256 d128 64 rows and four
+// ranges 75 + 4 us, two 98 + 4.
 FlashPlan flash_plan(const FlashShape& s, bool tree) {
   FlashPlan p{};
   const long long BH = s.BH(), R = (long long)s.G() * s.T, cus = device_cus();
-  p.rows = s.f32 || R <= 64 ? 64 : 128;
-  const int bn = s.f32 ? 32 : BN;
-  const long long nb = (R + p.rows - 1) / p.rows * BH;
-  const long long ntiles = (s.M + bn - 1) / bn + (s.T + bn - 1) / bn;
-  long long ns = (2 * cus + nb - 1) / nb;
-  if (ns > ntiles / 2) ns = ntiles / 2;
-  if (ns > kMaxFlashSplit) ns = kMaxFlashSplit;
-  p.nsplit = ns < 1 ? 1 : (int)ns;
+  const long long ntiles = (s.M + BN - 1) / BN + (s.T + BN - 1) / BN;
+  struct Block { int rows, resident; double us[4]; };
+  static const Block k128[] = {{64, 3, {0.75, 1.13, 1.57}}, {128, 2, {1.05, 1.6}}, {256, 1, {1.4}}};
+  static const Block k64[] = {{64, 4, {0.62, 0.87, 1.11, 1.41}}, {128, 3, {0.86, 1.21, 1.58}},
+                              {256, 1, {1.02}}};
+  // float32: 64 rows, two blocks per CU, 16 times the products' time
+  static const Block kF32[] = {{64, 2, {4.0, 5.5}}};
+  const Block* const blocks = s.f32 ? kF32 : s.d == 64 ? k64 : k128;
+  double best = INFINITY;
+  for (int v = 0; v < (s.f32 ? 1 : 3); ++v) {
+    const Block& k = blocks[v];
+    const long long nb = (R + k.rows - 1) / k.rows * BH, round = cus * k.resident;
+    for (int n = 1; n <= kMaxFlashSplit && (n == 1 || n <= ntiles / 2); ++n) {
+      const long long full = nb * n / round, left = (nb * n % round + cus - 1) / cus;
+      const double tiles = (double)((ntiles + n - 1) / n);
+      double us = tiles * (full * k.us[k.resident - 1] + (left ? k.us[left - 1] : 0.0)) +
+                  5.0 * (double)(full + (left != 0));
+      if (n > 1) us += 3.0 + (double)n * (double)BH * (double)R * s.d * 4.0 / 3.0e6;
+      if (us < 0.97 * best) {   // a clear gain for more ranges or rows
+        best = us;
+        p.rows = k.rows;
+        p.nsplit = n;
+      }
+    }
+  }
   p.nranges = column_ranges(s, s.T);
   size_t off = 0;
   p.off_stats = off;
@@ -636,11 +750,18 @@ FlashPlan flash_plan(const FlashShape& s, bool tree) {
   return p;
 }
 
+// Waves per block of the bf16 column sums (32 keys each): 8, whose blocks read the
+// rows half as often, where such blocks give every CU two.
+int column_waves(const FlashShape& s, int ncol) {
+  const long long nb = (long long)((s.M + 255) / 256 + (ncol + 255) / 256) * s.BH();
+  return (long long)s.G() * ncol >= 512 && nb * 4 >= device_cus() ? 8 : 4;
+}
+
 int column_ranges(const FlashShape& s, int ncol) {
-  const int kb = s.f32 ? kColumnKeysF32 : kColumnKeys;
+  const int kb = s.f32 ? kColumnKeysF32 : 32 * column_waves(s, ncol);
   const long long nb = (long long)((s.M + kb - 1) / kb + (ncol + kb - 1) / kb) * s.BH();
   const long long steps = ((long long)s.G() * ncol + kQRows - 1) / kQRows;
-  long long n = (2ll * device_cus() + nb - 1) / nb;
+  long long n = (4ll * device_cus() + nb - 1) / nb;
   if (n > steps / 4) n = steps / 4;
   if (n > kMaxColumnRanges) n = kMaxColumnRanges;
   return n < 1 ? 1 : (int)n;
@@ -661,8 +782,10 @@ hipError_t launch_flash_combine(const FlashShape& s, const FlashPlan& p, void* o
   const size_t rows = (size_t)s.BH() * s.G() * s.T;
   auto go = [&](auto D, auto e) {
     typedef decltype(e) E;
-    constexpr int per = kThreads / (decltype(D)::value / 4);
-    return launch_kernel(K_FLASH_COMBINE, flash_combine<decltype(D)::value, E>,
+    constexpr int kD = decltype(D)::value;
+    const bool few = p.nsplit <= kFewSplits;
+    const int per = kThreads / (kD / 4) / (few ? 1 : 8);
+    return launch_kernel(K_FLASH_COMBINE, few ? flash_combine<kD, E, 1> : flash_combine<kD, E, 8>,
                          dim3((unsigned)((rows + per - 1) / per)), dim3(kThreads), st,
                          reinterpret_cast<const float2*>(ws + p.off_stats),
                          reinterpret_cast<const float*>(ws + p.off_opart), (E*)out, lse, s.BH(),
@@ -690,13 +813,18 @@ hipError_t launch_flash(const FlashShape& s, const FlashPlan& p, const FlashIn& 
     constexpr int kD = decltype(D)::value;
     constexpr bool kQ = decltype(q)::value;
     auto go = [&](auto kern) {
-      return launch_kernel(K_FLASH, kern, grid, dim3(kThreads), st, a, p.nsplit, (bf16_t*)out, lse,
+      return launch_kernel(K_FLASH, kern, grid, dim3(p.rows == 256 ? 512 : 256), st, a, p.nsplit,
+                           (bf16_t*)out, lse,
                            stats, opart);
     };
-    if (tree)
-      return p.rows == 128 ? go(flash_pass<kD, kQ, true, 2>) : go(flash_pass<kD, kQ, true, 1>);
-    if constexpr (kQ)
-      return p.rows == 128 ? go(flash_pass<kD, true, false, 2>) : go(flash_pass<kD, true, false, 1>);
+    auto rows = [&](auto mask) {
+      constexpr bool kT = decltype(mask)::value;
+      return p.rows == 256   ? go(flash_pass<kD, kQ, kT, 2, 8>)
+             : p.rows == 128 ? go(flash_pass<kD, kQ, kT, 2, 4>)
+                             : go(flash_pass<kD, kQ, kT, 1, 4>);
+    };
+    if (tree) return rows(IntConst<1>{});
+    if constexpr (kQ) return rows(IntConst<0>{});
     return hipErrorInvalidValue;   // the chunk over a bf16 cache has its own kernels
   });
   if (e != hipSuccess || p.nsplit == 1) return e;
@@ -708,21 +836,19 @@ hipError_t launch_columns(const FlashShape& s, const FlashPlan& p, const FlashIn
                           float* wsum, char* ws, float scale, hipStream_t st) {
   const Args a = make_args(s, in, ws, p, scale);
   float* parts = reinterpret_cast<float*>(ws + p.off_parts);
-  const int ncol = path ? A : s.T;
-  const int kb = kColumnKeys, tiles = (s.M + kb - 1) / kb + (ncol + kb - 1) / kb;
-  const int ncopy = path ? (A * (s.d / 8) + kThreads - 1) / kThreads : 0;
+  const int ncol = path ? A : s.T, nw = column_waves(s, ncol);
+  const int kb = 32 * nw, nt = 64 * nw, tiles = (s.M + kb - 1) / kb + (ncol + kb - 1) / kb;
+  const int ncopy = path ? (A * (s.d / 8) + nt - 1) / nt : 0;
   const ColArgs c{lse, path, ncol, s.G() * ncol, p.nranges > 1 ? parts : wsum, (bf16_t*)k_acc,
                   (bf16_t*)v_acc, ncopy};
   const dim3 grid(tiles + ncopy, s.BH(), p.nranges);
   const hipError_t e = with_cache(s.d, in.q8, [&](auto D, auto q) {
     constexpr int kD = decltype(D)::value;
     constexpr bool kQ = decltype(q)::value;
-    constexpr int kN = kColumnKeys / (16 * kWaves);
-    auto go = [&](auto kern) {
-      return launch_kernel(K_COLUMNS, kern, grid, dim3(kThreads), st, a, c);
-    };
-    if (path) return go(column_pass<kD, kQ, true, kN>);
-    if constexpr (kQ) return go(column_pass<kD, true, false, kN>);
+    auto go = [&](auto kern) { return launch_kernel(K_COLUMNS, kern, grid, dim3(nt), st, a, c); };
+    if (path) return nw == 8 ? go(column_pass<kD, kQ, true, 2, 8>) : go(column_pass<kD, kQ, true, 2, 4>);
+    if constexpr (kQ)
+      return nw == 8 ? go(column_pass<kD, true, false, 2, 8>) : go(column_pass<kD, true, false, 2, 4>);
     return hipErrorInvalidValue;
   });
   if (e != hipSuccess || p.nranges == 1) return e;

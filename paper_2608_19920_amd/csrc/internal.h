@@ -335,9 +335,10 @@ struct FlashPlan {
   size_t off_stats, off_opart, off_bits, off_parts, bytes;
 };
 constexpr int kMaxFlashSplit = 32, kMaxColumnRanges = 8;
-constexpr int kColumnKeys = 128, kColumnKeysF32 = 64;   // keys per block of the column sums
+constexpr int kColumnKeysF32 = 64;   // keys per block of the float32 column sums
 FlashPlan flash_plan(const FlashShape& s, bool tree);
 int column_ranges(const FlashShape& s, int ncol);
+int column_waves(const FlashShape& s, int ncol);
 // tree: the mask of the ancestor bits that launch_tree_bits left in ws.
 hipError_t launch_flash(const FlashShape& s, const FlashPlan& p, const FlashIn& in, bool tree,
                         void* out, float* lse, char* ws, float scale, hipStream_t st);
