@@ -1012,7 +1012,7 @@ hipError_t launch_attend_q8(const void* q, const CacheQ8& c, const void* k_new, 
   const FlashShape s{B, Hq, Hkv, T, M, d, dtype == H2O_F32};
   const FlashPlan p = flash_plan(s, false);
   const FlashIn in{true, q, c.k, c.v, c.ks, c.vs, k_new, v_new};
-  hipError_t e = (s.f32 ? launch_flash_f32 : launch_flash)(s, p, in, false, out, lse, ws, scale, st);
+  hipError_t e = (s.f32 ? launch_flash_f32 : launch_flash)(s, p, in, out, lse, ws, scale, st);
   if (e != hipSuccess) return e;
   return (s.f32 ? launch_columns_f32 : launch_columns)(s, p, in, lse, nullptr, 0, nullptr, nullptr,
                                                        wsum, ws, scale, st);
@@ -1205,11 +1205,9 @@ int h2o_sdpa_tree(const void* q, const void* k_cache, const float* k_scales, con
   char* ws = reinterpret_cast<char*>(workspace);
   const FlashShape s{B, Hq, Hkv, T, M, d, dtype == H2O_F32};
   const FlashPlan p = flash_plan(s, true);
-  const FlashIn in{k_scales != nullptr, q, k_cache, v_cache, k_scales, v_scales, k_new, v_new};
-  hipError_t e = launch_tree_bits(s, p, parents, ws, st);
-  if (e == hipSuccess)
-    e = (s.f32 ? launch_flash_f32 : launch_flash)(s, p, in, true, out, lse, ws, scale, st);
-  return launched(e);
+  const FlashIn in{k_scales != nullptr, q,     k_cache, v_cache, k_scales,
+                   v_scales,            k_new, v_new,   parents};
+  return launched((s.f32 ? launch_flash_f32 : launch_flash)(s, p, in, out, lse, ws, scale, st));
 }
 
 int h2o_tree_accept(const void* q, const void* k_cache, const float* k_scales, const void* k_new,

@@ -30,8 +30,8 @@ using namespace mfma;
 
 constexpr int BN = 32;          // keys per tile
 constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
 constexpr int kXcds = 8;
+constexpr int kWaveTree = 64;   // nodes of a tree that a wave masks by itself
 constexpr int kFewSplits = 4;   // key ranges that one thread merges alone
 // A lambda over register arrays: a call that is not inlined would put them in memory.
 #define H2O_INLINE __attribute__((always_inline))
@@ -43,7 +43,9 @@ struct Args {
   const void *kc, *vc;          // [BH][M][D], bf16 or codes
   const float *ks, *vs;         // [BH][M], 8-bit cache
   const bf16_t *kn, *vn;        // [BH][T][D]
-  const uint32_t* bits;         // tree: [B][T][W] ancestor bits, a node's own among them
+  const int32_t* parents;       // tree: [B][T]
+  const uint32_t* bits;         // tree of more than 64 nodes: [B][T][W] ancestor bits, a
+                                // node's own among them
   int Hq, Hkv, G, T, M, R, W;
   float c;                      // scale * log2(e)
 };
@@ -216,6 +218,24 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
     for (int db = 0; db < D / 16; ++db) oacc[db][n] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
+  // A tree of at most 64 nodes: lane i follows node i up by doubling its way, and a
+  // row's lanes take the node's bits.
+  uint64_t own[NQB];
+  if (TREE && a.T <= kWaveTree) {
+    int up = lane < a.T ? a.parents[(size_t)b * a.T + lane] : -1;
+    if (up < 0 || up >= lane) up = -1;
+    uint64_t mine = 1ull << lane;
+#pragma unroll 1
+    for (int reach = 1; reach < a.T; reach *= 2) {
+      const uint64_t more = __shfl(mine, up < 0 ? lane : up, 64);
+      const int next = __shfl(up, up < 0 ? lane : up, 64);
+      mine |= more;
+      up = up < 0 ? -1 : next;
+    }
+#pragma unroll
+    for (int n = 0; n < NQB; ++n) own[n] = __shfl(mine, qi[n], 64);
+  }
+
   // Tile t, in LDS at K, V, scl: scores, probabilities, O += P V; then the registers g,
   // with tile t + 1, go to the other buffer, and tile t + 2 is requested into them.
   auto tile = [&](auto masked, auto whole, int t, const bf16_t* K, const bf16_t* V,
@@ -238,7 +258,9 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
     uint32_t seen[NQB];
     if (MASK && TREE && !cache)
 #pragma unroll
-      for (int n = 0; n < NQB; ++n) seen[n] = a.bits[((size_t)b * a.T + qi[n]) * a.W + (t - tc)];
+      for (int n = 0; n < NQB; ++n)
+        seen[n] = a.T <= kWaveTree ? (uint32_t)(own[n] >> (t > tc ? 32 : 0))
+                                   : a.bits[((size_t)b * a.T + qi[n]) * a.W + (t - tc)];
     f32x4 cks[2], cvs[2];
     if (Q8)
 #pragma unroll
@@ -490,8 +512,9 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void column_pass(Args a, 
   const int j0 = (cache ? bx : bx - tc) * KB + wave * NKB * 16;
   const int nkeys = cache ? a.M : p.A;
   // this lane's operand rows: key j0 + 16 kb + l16, elements 64 x + 16 g4 .. +15
-  // (an order of d that both operands share; 16 codes are one load)
-  bf16x8 kf[NKB][D / 32];
+  // (an order of d that both operands share; 16 codes are one load). All that the
+  // block reads first is requested before any of it is used.
+  u32x4 kr[NKB][D / 32];
   f32x4 cks[NKB], cs[NKB];
 #pragma unroll
   for (int kb = 0; kb < NKB; ++kb) {
@@ -499,25 +522,19 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void column_pass(Args a, 
     if (Q8 && cache) {
       const int8_t* src = (const int8_t*)a.kc + (bh * a.M + j) * (size_t)D + 16 * g4;
 #pragma unroll
-      for (int x = 0; x < D / 64; ++x) {
-        const u32x4 v = *reinterpret_cast<const u32x4*>(src + 64 * x);
-        kf[kb][2 * x] = q8::codes_bf16(v[0], v[1]);
-        kf[kb][2 * x + 1] = q8::codes_bf16(v[2], v[3]);
-      }
+      for (int x = 0; x < D / 64; ++x) kr[kb][x] = *reinterpret_cast<const u32x4*>(src + 64 * x);
     } else {
       const int n = cache ? j : max(node_of(j), 0);
       const bf16_t* src = (cache ? (const bf16_t*)a.kc + (bh * a.M + n) * (size_t)D
                                  : a.kn + (bh * a.T + n) * (size_t)D) + 16 * g4;
 #pragma unroll
-      for (int x = 0; x < D / 64; ++x) {
-        kf[kb][2 * x] = *reinterpret_cast<const bf16x8*>(src + 64 * x);
-        kf[kb][2 * x + 1] = *reinterpret_cast<const bf16x8*>(src + 64 * x + 8);
-      }
+      for (int x = 0; x < D / 32; ++x)
+        kr[kb][x] = *reinterpret_cast<const u32x4*>(src + 64 * (x >> 1) + 8 * (x & 1));
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int jr = min(j0 + 16 * kb + 4 * g4 + r, nkeys - 1);
-      cks[kb][r] = Q8 && cache ? a.ks[bh * a.M + jr] * a.c : a.c;
+      cks[kb][r] = Q8 && cache ? a.ks[bh * a.M + jr] : 1.f;
       cs[kb][r] = 0.f;
     }
   }
@@ -574,6 +591,22 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void column_pass(Args a, 
       pos[buf][tid] = ir;
     }
   };
+  if (s0 < s1) load();
+  bf16x8 kf[NKB][D / 32];
+#pragma unroll
+  for (int kb = 0; kb < NKB; ++kb) {
+    cks[kb] *= a.c;
+    if (Q8 && cache) {
+#pragma unroll
+      for (int x = 0; x < D / 64; ++x) {
+        kf[kb][2 * x] = q8::codes_bf16(kr[kb][x][0], kr[kb][x][1]);
+        kf[kb][2 * x + 1] = q8::codes_bf16(kr[kb][x][2], kr[kb][x][3]);
+      }
+    } else {
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x) kf[kb][x] = __builtin_bit_cast(bf16x8, kr[kb][x]);
+    }
+  }
   // the products of the next 16 rows go out before the exponentials of these
   auto step = [&](auto chunk, int buf) H2O_INLINE {
     f32x4 s[2][NKB];
@@ -605,7 +638,6 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void column_pass(Args a, 
     }
   };
   if (s0 < s1) {
-    load();
     store(0);
     if (s0 + 1 < s1) load();
     __syncthreads();
@@ -690,7 +722,7 @@ hipError_t with_cache(int d, bool q8, F&& f) {
 Args make_args(const FlashShape& s, const FlashIn& in, const char* ws, const FlashPlan& p,
                float scale) {
   return Args{(const bf16_t*)in.q, in.kc, in.vc, in.ks, in.vs, (const bf16_t*)in.kn,
-              (const bf16_t*)in.vn, reinterpret_cast<const uint32_t*>(ws + p.off_bits), s.Hq, s.Hkv,
+              (const bf16_t*)in.vn, in.parents, reinterpret_cast<const uint32_t*>(ws + p.off_bits), s.Hq, s.Hkv,
               s.G(), s.T, s.M, s.G() * s.T, (s.T + 31) / 32, scale * kLog2e};
 }
 
@@ -740,7 +772,8 @@ FlashPlan flash_plan(const FlashShape& s, bool tree) {
   p.off_opart = off;
   if (p.nsplit > 1) off = align256_size(off + (size_t)p.nsplit * BH * R * s.d * sizeof(float));
   p.off_bits = off;
-  if (tree) off = align256_size(off + (size_t)s.B * s.T * ((s.T + 31) / 32) * 4);
+  if (tree && (s.f32 || s.T > kWaveTree))
+    off = align256_size(off + (size_t)s.B * s.T * ((s.T + 31) / 32) * 4);
   // the tree's column sums are a call of their own, of any path
   p.off_parts = tree ? 0 : off;
   const int nr = tree ? kMaxColumnRanges : p.nranges;
@@ -757,12 +790,15 @@ int column_waves(const FlashShape& s, int ncol) {
   return (long long)s.G() * ncol >= 512 && nb * 4 >= device_cus() ? 8 : 4;
 }
 
+// Row ranges of the column sums: blocks for four per CU, at least two steps each, and
+// only from eight steps on (a step takes 0.8 us in bf16 and 1.1 in float32, adding the
+// ranges 4: B1 Hq16 Hkv4 d64 M2049 T131 in float32 23.8 us in one range, 12.7 + 4 in four).
 int column_ranges(const FlashShape& s, int ncol) {
-  const int kb = s.f32 ? kColumnKeysF32 : 32 * column_waves(s, ncol);
+  const int kb = s.f32 ? kColumnKeysF32 : 32 * column_waves(s, ncol), qr = s.f32 ? 32 : kQRows;
   const long long nb = (long long)((s.M + kb - 1) / kb + (ncol + kb - 1) / kb) * s.BH();
-  const long long steps = ((long long)s.G() * ncol + kQRows - 1) / kQRows;
-  long long n = (4ll * device_cus() + nb - 1) / nb;
-  if (n > steps / 4) n = steps / 4;
+  const long long steps = ((long long)s.G() * ncol + qr - 1) / qr;
+  long long n = steps < 8 ? 1 : (4ll * device_cus() + nb - 1) / nb;
+  if (n > steps / 2) n = steps / 2;
   if (n > kMaxColumnRanges) n = kMaxColumnRanges;
   return n < 1 ? 1 : (int)n;
 }
@@ -802,8 +838,13 @@ hipError_t launch_column_reduce(const float* parts, float* wsum, size_t n, int n
                        wsum, n, nranges);
 }
 
-hipError_t launch_flash(const FlashShape& s, const FlashPlan& p, const FlashIn& in, bool tree,
-                        void* out, float* lse, char* ws, float scale, hipStream_t st) {
+hipError_t launch_flash(const FlashShape& s, const FlashPlan& p, const FlashIn& in, void* out,
+                        float* lse, char* ws, float scale, hipStream_t st) {
+  const bool tree = in.parents != nullptr;
+  if (tree && s.T > kWaveTree) {
+    const hipError_t e = launch_tree_bits(s, p, in.parents, ws, st);
+    if (e != hipSuccess) return e;
+  }
   const Args a = make_args(s, in, ws, p, scale);
   const int nrt = (a.R + p.rows - 1) / p.rows;
   const dim3 grid(nrt * p.nsplit, s.BH());

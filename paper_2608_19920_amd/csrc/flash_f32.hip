@@ -120,9 +120,9 @@ __global__ __launch_bounds__(kThreads) void flash_f32(Args a, int nsplit, float*
                                                       float2* __restrict__ stats,
                                                       float* __restrict__ opart) {
   constexpr int ROWS = kWaves * 16, P = lds_pitch(D), NK = BN / 16;
-  __shared__ __attribute__((aligned(16))) float Ks[BN * P];
-  __shared__ __attribute__((aligned(16))) float Vs[BN * P];
-  __shared__ int odd[2];            // by tile parity: it holds a value that is not finite
+  __shared__ __attribute__((aligned(16))) float Ks2[2][BN * P];
+  __shared__ __attribute__((aligned(16))) float Vs2[2][BN * P];
+  __shared__ int odd[3];            // by tile: it holds a value that is not finite
   const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nrt = gridDim.x / nsplit, rt = nrt - 1 - (int)blockIdx.x % nrt;
@@ -146,15 +146,31 @@ __global__ __launch_bounds__(kThreads) void flash_f32(Args a, int nsplit, float*
     for (int u = 0; u < 4; ++u) acc[x][u] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
   Regs<D, Q8> g;
-  if (t0 < t1) load_tile<D, Q8>(g, a, bh, t0, tc);
-  if (threadIdx.x < 2) odd[threadIdx.x] = 0;
+  // two LDS buffers, one barrier a tile: tile t + 1 goes from registers to the other
+  // buffer, and tile t + 2 is requested, before tile t is used. The flag of a tile is
+  // cleared two barriers before it can be set.
+  auto put = [&](int t) {
+    const bool bad = store_tile<D, Q8>(Ks2[(t - t0) & 1], Vs2[(t - t0) & 1], g, t, tc);
+    if (bad && t >= tc) odd[(t - t0) % 3] = 1;
+  };
+  if (threadIdx.x < 3) odd[threadIdx.x] = 0;
+  __syncthreads();
+  if (t0 < t1) {
+    load_tile<D, Q8>(g, a, bh, t0, tc);
+    put(t0);
+    if (t0 + 1 < t1) load_tile<D, Q8>(g, a, bh, t0 + 1, tc);
+  }
   for (int t = t0; t < t1; ++t) {
     const bool cache = t < tc;
-    __syncthreads();                // tile t - 1 is used up, and its flag
-    if (threadIdx.x == 0) odd[(t + 1) & 1] = 0;
-    if (store_tile<D, Q8>(Ks, Vs, g, t, tc) && !cache) odd[t & 1] = 1;
-    if (t + 1 < t1) load_tile<D, Q8>(g, a, bh, t + 1, tc);
-    __syncthreads();
+    __syncthreads();                // tile t is in LDS, tile t - 1 used up
+    if (threadIdx.x == 0) odd[(t - t0 + 2) % 3] = 0;
+    const float* Ks = Ks2[(t - t0) & 1];
+    const float* Vs = Vs2[(t - t0) & 1];
+    const bool finite = !odd[(t - t0) % 3];
+    if (t + 1 < t1) {
+      put(t + 1);
+      if (t + 2 < t1) load_tile<D, Q8>(g, a, bh, t + 2, tc);
+    }
     const uint32_t seen = TREE && !cache ? a.bits[((size_t)b * a.T + i) * a.W + (t - tc)] : 0u;
     f32x4 s[NK];
     uint32_t hidden = 0u;
@@ -197,7 +213,7 @@ __global__ __launch_bounds__(kThreads) void flash_f32(Args a, int nsplit, float*
         s[kb][e] = __builtin_amdgcn_exp2f(s[kb][e] - mu);
         l += s[kb][e];
       }
-    if (!odd[t & 1]) {   // block-uniform
+    if (finite) {   // block-uniform
 #pragma unroll
       for (int kb = 0; kb < NK; ++kb)
 #pragma unroll
@@ -259,8 +275,9 @@ constexpr int kQRows = 32;
 template <int D, bool Q8, bool PATH>
 __global__ __launch_bounds__(kThreads) void column_f32(Args a, ColArgs p) {
   constexpr int KB = kWaves * 16, P = lds_pitch(D), NU = kQRows * D / 4 / kThreads;
-  __shared__ __attribute__((aligned(16))) float Qs[kQRows * P];
-  __shared__ float lam[kQRows];
+  __shared__ __attribute__((aligned(16))) float Qs[2][kQRows * P];
+  __shared__ float lam[2][kQRows];
+  __shared__ int pos[2][kQRows];
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const size_t bh = blockIdx.y;
@@ -310,49 +327,85 @@ __global__ __launch_bounds__(kThreads) void column_f32(Args a, ColArgs p) {
   const int steps = (p.R + kQRows - 1) / kQRows;
   const int per = (steps + (int)gridDim.z - 1) / (int)gridDim.z;
   const int s1 = min(steps, ((int)blockIdx.z + 1) * per), s0 = max(first, (int)blockIdx.z * per);
+  // rows as in column_pass: stepped without a division, past the last row kept at it
+  constexpr int RU = kThreads / (D / 4);
   f32x4 qr[NU];
   float lr = 0.f;
-  auto load = [&](int s) {
+  int ir = 0, ri[NU], rg[NU], li, lg;
+  const int part = 4 * (tid % (D / 4)), di = kQRows / a.G, dg = kQRows % a.G;
+#pragma unroll
+  for (int e = 0; e < NU; ++e) {
+    const int r = s0 * kQRows + tid / (D / 4) + e * RU;
+    ri[e] = r / a.G;
+    rg[e] = r % a.G;
+  }
+  li = (s0 * kQRows + tid) / a.G;
+  lg = (s0 * kQRows + tid) % a.G;
+  const float* qh = a.q + (size_t)(b * a.Hq + h * a.G) * a.T * D + part;
+  const float* lh = p.lse + (size_t)(b * a.Hq + h * a.G) * a.T;
+  auto advance = [&](int& i, int& g) {
+    i += di;
+    g += dg;
+    if (g >= a.G) { g -= a.G; ++i; }
+  };
+  auto load = [&]() {   // the rows of the next step
 #pragma unroll
     for (int e = 0; e < NU; ++e) {
-      const int u = tid + e * kThreads, r = min(s * kQRows + u / (D / 4), p.R - 1);
-      const int n = max(node_of(r / a.G), 0);
-      qr[e] = load4(a.q + ((size_t)(b * a.Hq + h * a.G + r % a.G) * a.T + n) * D + 4 * (u % (D / 4)));
+      const int n = max(node_of(min(ri[e], p.A - 1)), 0);
+      qr[e] = load4(qh + (uint32_t)(rg[e] * a.T + n) * (uint32_t)D);
+      advance(ri[e], rg[e]);
     }
     if (tid < kQRows) {
-      const int r = s * kQRows + tid, n = r < p.R ? node_of(r / a.G) : -1;
-      lr = n >= 0 ? p.lse[(size_t)(b * a.Hq + h * a.G + r % a.G) * a.T + n] * kLog2e : INFINITY;
+      const int n = li < p.A ? node_of(li) : -1;
+      lr = n >= 0 ? lh[lg * a.T + n] * kLog2e : INFINITY;
+      ir = li;
+      advance(li, lg);
     }
   };
-  if (s0 < s1) load(s0);
-  for (int s = s0; s < s1; ++s) {
-    __syncthreads();
+  auto store = [&](int buf) {
 #pragma unroll
-    for (int e = 0; e < NU; ++e) {
-      const int u = tid + e * kThreads;
-      *reinterpret_cast<f32x4*>(&Qs[u / (D / 4) * P + 4 * (u % (D / 4))]) = qr[e];
+    for (int e = 0; e < NU; ++e)
+      *reinterpret_cast<f32x4*>(&Qs[buf][(tid / (D / 4) + e * RU) * P + part]) = qr[e];
+    if (tid < kQRows) {
+      lam[buf][tid] = lr;
+      pos[buf][tid] = ir;
     }
-    if (tid < kQRows) lam[tid] = lr;
-    if (s + 1 < s1) load(s + 1);
+  };
+  if (s0 < s1) {
+    load();
+    store(0);
+    if (s0 + 1 < s1) load();
     __syncthreads();
+  }
+  for (int s = s0; s < s1; ++s) {
+    const int buf = (s - s0) & 1;
+    if (s + 1 < s1) {
+      store(buf ^ 1);
+      if (s + 2 < s1) load();
+    }
+    f32x4 w[kQRows / 16];
+#pragma unroll
+    for (int n = 0; n < kQRows / 16; ++n) w[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x)
+#pragma unroll
+      for (int n = 0; n < kQRows / 16; ++n) {
+        const f32x4 qf = load4(&Qs[buf][(16 * n + l16) * P + 16 * x + 4 * g4]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) w[n] = mma4(kf[x][u], qf[u], w[n]);
+      }
 #pragma unroll
     for (int n = 0; n < kQRows / 16; ++n) {
-      f32x4 w = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int x = 0; x < D / 16; ++x) {
-        const f32x4 qf = load4(&Qs[(16 * n + l16) * P + 16 * x + 4 * g4]);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) w = mma4(kf[x][u], qf[u], w);
-      }
-      const float la = lam[16 * n + l16];
-      const int i = (s * kQRows + 16 * n + l16) / a.G;
+      const float la = lam[buf][16 * n + l16];
+      const int i = pos[buf][16 * n + l16];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(w[r], a.c, -la));
+        const float x = __builtin_amdgcn_exp2f(fmaf(w[n][r], a.c, -la));
         const bool hid = la == INFINITY || (!cache && j0 + 4 * g4 + r > i);
         cs[r] += hid ? 0.f : x;
       }
     }
+    __syncthreads();
   }
   float* dst = p.dst + ((size_t)blockIdx.z * gridDim.y + bh) * (a.M + p.A) + (cache ? 0 : a.M);
 #pragma unroll
@@ -379,8 +432,13 @@ Args make_args(const FlashShape& s, const FlashIn& in, const char* ws, const Fla
 
 }  // namespace
 
-hipError_t launch_flash_f32(const FlashShape& s, const FlashPlan& p, const FlashIn& in, bool tree,
-                            void* out, float* lse, char* ws, float scale, hipStream_t st) {
+hipError_t launch_flash_f32(const FlashShape& s, const FlashPlan& p, const FlashIn& in, void* out,
+                            float* lse, char* ws, float scale, hipStream_t st) {
+  const bool tree = in.parents != nullptr;
+  if (tree) {
+    const hipError_t e = launch_tree_bits(s, p, in.parents, ws, st);
+    if (e != hipSuccess) return e;
+  }
   const Args a = make_args(s, in, ws, p, scale);
   const dim3 grid((a.R + p.rows - 1) / p.rows * p.nsplit, s.BH());
   float2* stats = reinterpret_cast<float2*>(ws + p.off_stats);

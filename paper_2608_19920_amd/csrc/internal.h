@@ -327,6 +327,7 @@ struct FlashIn {
   const void *q, *kc, *vc;
   const float *ks, *vs;
   const void *kn, *vn;
+  const int32_t* parents = nullptr;   // [B][T]: the chunk is a tree
 };
 struct FlashPlan {
   int rows;                     // packed rows per block
@@ -339,11 +340,10 @@ constexpr int kColumnKeysF32 = 64;   // keys per block of the float32 column sum
 FlashPlan flash_plan(const FlashShape& s, bool tree);
 int column_ranges(const FlashShape& s, int ncol);
 int column_waves(const FlashShape& s, int ncol);
-// tree: the mask of the ancestor bits that launch_tree_bits left in ws.
-hipError_t launch_flash(const FlashShape& s, const FlashPlan& p, const FlashIn& in, bool tree,
-                        void* out, float* lse, char* ws, float scale, hipStream_t st);
-hipError_t launch_flash_f32(const FlashShape& s, const FlashPlan& p, const FlashIn& in, bool tree,
-                            void* out, float* lse, char* ws, float scale, hipStream_t st);
+hipError_t launch_flash(const FlashShape& s, const FlashPlan& p, const FlashIn& in, void* out,
+                        float* lse, char* ws, float scale, hipStream_t st);
+hipError_t launch_flash_f32(const FlashShape& s, const FlashPlan& p, const FlashIn& in, void* out,
+                            float* lse, char* ws, float scale, hipStream_t st);
 hipError_t launch_flash_combine(const FlashShape& s, const FlashPlan& p, void* out, float* lse,
                                 const char* ws, hipStream_t st);
 hipError_t launch_tree_bits(const FlashShape& s, const FlashPlan& p, const int32_t* parents,

@@ -2,10 +2,11 @@
 // (row format and rounding: q8.h).
 //
 // Bound by memory: a row of d values is read once (2 d or 4 d bytes) and d + 4
-// bytes are written, or the reverse. Lane l of the d / 16 lanes that share a row
-// has 16 consecutive values of K and the same of V: 16-byte loads and stores of
-// both tensors in flight together, the row's maximum by exchanges between its
-// lanes, no LDS and no barrier.
+// bytes are written, or the reverse. A lane has kPer consecutive values of K and the
+// same of V, 32 bytes each: loads and stores of both tensors in flight together, the
+// row's maximum by exchanges between its lanes, no LDS and no barrier. (Float32 with 16
+// values a lane, 64 bytes: B3 Hkv16 d64, 3,001 rows written and read back 49 us, with 8
+// QF32.) B4 Hkv8 d128 bf16, 32,768 rows: 300 us for both calls, 5.4 TB/s.
 #include "internal.h"
 #include "q8.h"
 
@@ -28,30 +29,52 @@ struct InsertArgs {
   int32_t pos0;
 };
 
+template <typename E>
+__host__ __device__ constexpr int per_lane() { return 32 / (int)sizeof(E); }
+
+// N / 4 words of codes.
+template <int N>
+__device__ __forceinline__ void store_codes(int8_t* p, const uint32_t (&c)[N / 4]) {
+  if constexpr (N == 16) *reinterpret_cast<u32x4*>(p) = u32x4{c[0], c[1], c[2], c[3]};
+  else *reinterpret_cast<uint2*>(p) = make_uint2(c[0], c[1]);
+}
+template <int N>
+__device__ __forceinline__ void load_codes(uint32_t (&c)[N / 4], const int8_t* p) {
+  if constexpr (N == 16) {
+    const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = v[i];
+  } else {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    c[0] = v.x;
+    c[1] = v.y;
+  }
+}
+
 template <int D, typename E>
 __global__ __launch_bounds__(kThreads) void quantize_rows(
     const E* __restrict__ k_src, const E* __restrict__ v_src, const int32_t* __restrict__ idx,
     int8_t* __restrict__ kc, float* __restrict__ ks, int8_t* __restrict__ vc,
     float* __restrict__ vs, uint32_t nrows, int M, uint32_t k, InsertArgs ins) {
-  constexpr int LPR = D / 16;
+  constexpr int N = per_lane<E>(), LPR = D / N;
   const uint32_t row = blockIdx.x * (kThreads / LPR) + threadIdx.x / LPR;
   if (row >= nrows) return;   // whole rows: the lanes of a row leave together
   const int part = threadIdx.x % LPR;
   const uint32_t bh = row / k, i = row % k;
-  const size_t src = (size_t)row * D + 16 * part;
-  float x[16], y[16];
-  load_row<16>(x, k_src + src);
-  load_row<16>(y, v_src + src);
+  const size_t src = (size_t)row * D + N * part;
+  float x[N], y[N];
+  load_row<N>(x, k_src + src);
+  load_row<N>(y, v_src + src);
   const int slot = idx ? idx[row] : (int)i;
-  const float sx = row_scale(lanes_max<LPR>(amax_bits<16>(x)));
-  const float sy = row_scale(lanes_max<LPR>(amax_bits<16>(y)));
+  const float sx = row_scale(lanes_max<LPR>(amax_bits<N>(x)));
+  const float sy = row_scale(lanes_max<LPR>(amax_bits<N>(y)));
   if ((unsigned)slot >= (unsigned)M) return;
-  uint32_t cx[4], cy[4];
-  quantize<16>(x, sx, cx);
-  quantize<16>(y, sy, cy);
+  uint32_t cx[N / 4], cy[N / 4];
+  quantize<N>(x, sx, cx);
+  quantize<N>(y, sy, cy);
   const size_t dst = (size_t)bh * M + slot;
-  *reinterpret_cast<u32x4*>(kc + dst * D + 16 * part) = u32x4{cx[0], cx[1], cx[2], cx[3]};
-  *reinterpret_cast<u32x4*>(vc + dst * D + 16 * part) = u32x4{cy[0], cy[1], cy[2], cy[3]};
+  store_codes<N>(kc + dst * D + N * part, cx);
+  store_codes<N>(vc + dst * D + N * part, cy);
   if (part == 0) {
     ks[dst] = sx;
     vs[dst] = sy;
@@ -62,15 +85,17 @@ __global__ __launch_bounds__(kThreads) void quantize_rows(
   }
 }
 
-__device__ __forceinline__ void store_values(float* p, const u32x4& c, float s) {
+template <int N>
+__device__ __forceinline__ void store_values(float* p, const uint32_t (&c)[N / 4], float s) {
 #pragma unroll
-  for (int w = 0; w < 4; ++w)
+  for (int w = 0; w < N / 4; ++w)
     reinterpret_cast<f32x4*>(p)[w] =
         f32x4{code_f32(c[w], 0), code_f32(c[w], 1), code_f32(c[w], 2), code_f32(c[w], 3)} * s;
 }
-__device__ __forceinline__ void store_values(bf16_t* p, const u32x4& c, float s) {
+template <int N>
+__device__ __forceinline__ void store_values(bf16_t* p, const uint32_t (&c)[N / 4], float s) {
 #pragma unroll
-  for (int w = 0; w < 2; ++w) {
+  for (int w = 0; w < N / 8; ++w) {
     bf16x8 r;
 #pragma unroll
     for (int i = 0; i < 8; ++i) r[i] = (__bf16)(code_f32(c[2 * w + (i >> 2)], i & 3) * s);
@@ -83,18 +108,19 @@ __global__ __launch_bounds__(kThreads) void dequantize_rows(
     const int8_t* __restrict__ kc, const float* __restrict__ ks, const int8_t* __restrict__ vc,
     const float* __restrict__ vs, const int32_t* __restrict__ idx, E* __restrict__ k_dst,
     E* __restrict__ v_dst, uint32_t nrows, int M, uint32_t k) {
-  constexpr int LPR = D / 16;
+  constexpr int N = per_lane<E>(), LPR = D / N;
   const uint32_t row = blockIdx.x * (kThreads / LPR) + threadIdx.x / LPR;
   if (row >= nrows) return;
   const int part = threadIdx.x % LPR;
   const int slot = idx ? idx[row] : (int)(row % k);
   if ((unsigned)slot >= (unsigned)M) return;
-  const size_t src = (size_t)(row / k) * M + slot, dst = (size_t)row * D + 16 * part;
-  const u32x4 a = *reinterpret_cast<const u32x4*>(kc + src * D + 16 * part);
-  const u32x4 b = *reinterpret_cast<const u32x4*>(vc + src * D + 16 * part);
+  const size_t src = (size_t)(row / k) * M + slot, dst = (size_t)row * D + N * part;
+  uint32_t a[N / 4], b[N / 4];
+  load_codes<N>(a, kc + src * D + N * part);
+  load_codes<N>(b, vc + src * D + N * part);
   const float sa = ks[src], sb = vs[src];
-  store_values(k_dst + dst, a, sa);
-  store_values(v_dst + dst, b, sb);
+  store_values<N>(k_dst + dst, a, sa);
+  store_values<N>(v_dst + dst, b, sb);
 }
 
 template <typename F>
@@ -111,7 +137,7 @@ hipError_t launch_kv_quantize(const void* k_src, const void* v_src, const int32_
                               const float* wsum, int T, int32_t pos0) {
   const uint32_t n = (uint32_t)rows * (uint32_t)k;
   if (n == 0) return hipSuccess;
-  const uint32_t per = kThreads / (d / 16);
+  const uint32_t per = kThreads / (d / (f32 ? per_lane<float>() : per_lane<bf16_t>()));
   return with_form(d, f32, [&](auto D, auto e) {
     typedef decltype(e) E;
     return launch_kernel(K_KV_QUANT, quantize_rows<decltype(D)::value, E>, dim3((n + per - 1) / per),
@@ -124,7 +150,7 @@ hipError_t launch_kv_dequantize(const CacheQ8& c, const int32_t* idx, void* k_ds
                                 int rows, int M, int k, int d, bool f32, hipStream_t st) {
   const uint32_t n = (uint32_t)rows * (uint32_t)k;
   if (n == 0) return hipSuccess;
-  const uint32_t per = kThreads / (d / 16);
+  const uint32_t per = kThreads / (d / (f32 ? per_lane<float>() : per_lane<bf16_t>()));
   return with_form(d, f32, [&](auto D, auto e) {
     typedef decltype(e) E;
     return launch_kernel(K_KV_QUANT, dequantize_rows<decltype(D)::value, E>,
