@@ -467,9 +467,31 @@ struct ColArgs {
   int A, R;                     // chunk key columns and packed rows
   float* dst;                   // [ranges of rows][BH][M + A]
   bf16_t *k_acc, *v_acc;        // path: [BH][A][D], the path's keys and values
-  int ncopy;                    // blocks that copy them
 };
 constexpr int kQRows = 64;      // rows per step
+constexpr int kFewRows = 64;    // rows that a wave keeps (column_few)
+
+// Node of the path's entry (or, path null, chunk position) i, -1 if it is none.
+__device__ __forceinline__ int path_node(const int32_t* path, int i, int T) {
+  if (!path) return i;
+  const int n = path[i];
+  return (unsigned)n < (unsigned)T ? n : -1;
+}
+// Unit e of the path's keys and values, 16 bytes.
+template <int D>
+__device__ __forceinline__ void copy_path(const Args& a, const ColArgs& p, size_t bh,
+                                          const int32_t* path, int e) {
+  const int i = e / (D / 8), c = e % (D / 8);
+  if (i >= p.A) return;
+  const int n = path_node(path, i, a.T);
+  u32x4 kv = {0u, 0u, 0u, 0u}, vv = kv;
+  if (n >= 0) {
+    kv = reinterpret_cast<const u32x4*>(a.kn + (bh * a.T + n) * (size_t)D)[c];
+    vv = reinterpret_cast<const u32x4*>(a.vn + (bh * a.T + n) * (size_t)D)[c];
+  }
+  reinterpret_cast<u32x4*>(p.k_acc + (bh * p.A + i) * (size_t)D)[c] = kv;
+  reinterpret_cast<u32x4*>(p.v_acc + (bh * p.A + i) * (size_t)D)[c] = vv;
+}
 
 template <int D, bool Q8, bool PATH, int NKB, int NW>
 __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void column_pass(Args a, ColArgs p) {
@@ -489,23 +511,9 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void column_pass(Args a, 
   const int b = bhi / a.Hkv, h = bhi % a.Hkv;
   const int tc = (a.M + KB - 1) / KB, tn = (p.A + KB - 1) / KB;
   const int32_t* path = PATH ? p.path + (size_t)b * p.A : nullptr;
-  // node of the chunk's key or row position i, -1 if it is none
-  auto node_of = [&](int i) {
-    if (!PATH) return i;
-    const int n = path[i];
-    return (unsigned)n < (unsigned)a.T ? n : -1;
-  };
-  if (PATH && bx >= tc + tn) {   // the path's rows, 16 bytes a thread
-    const int e = (bx - tc - tn) * NT + tid, i = e / (D / 8), c = e % (D / 8);
-    if (bz || i >= p.A) return;
-    const int n = node_of(i);
-    u32x4 kv = {0u, 0u, 0u, 0u}, vv = kv;
-    if (n >= 0) {
-      kv = reinterpret_cast<const u32x4*>(a.kn + (bh * a.T + n) * (size_t)D)[c];
-      vv = reinterpret_cast<const u32x4*>(a.vn + (bh * a.T + n) * (size_t)D)[c];
-    }
-    reinterpret_cast<u32x4*>(p.k_acc + (bh * p.A + i) * (size_t)D)[c] = kv;
-    reinterpret_cast<u32x4*>(p.v_acc + (bh * p.A + i) * (size_t)D)[c] = vv;
+  auto node_of = [&](int i) { return path_node(path, i, a.T); };
+  if (PATH && bx >= tc + tn) {   // the path's rows
+    if (!bz) copy_path<D>(a, p, bh, path, (bx - tc - tn) * NT + tid);
     return;
   }
   const bool cache = bx < tc;
@@ -664,6 +672,172 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void column_pass(Args a, 
       const int j = j0 + 16 * kb + 4 * g4 + r;
       if (l16 == 0 && j < nkeys) dst[j] = PATH && !cache && node_of(j) < 0 ? 0.f : v;
     }
+}
+
+// The column sums of at most 16 NR packed rows. The rows go into LDS once and the
+// keys stream past them, 32 a wave, each group requested before the last one is used,
+// without a barrier: bound by the cache's K rows, which are read once, where there are
+// many. (B4 Hkv8 G4 d128 M32768, 5 rows a head: 8-bit cache 35 us, bf16 62
+// (4.3 TB/s), against 72 and 79 by column_pass.)
+template <int D, bool Q8, bool PATH, int NR>
+__global__ __launch_bounds__(kThreads) void column_few(Args a, ColArgs p, int nb) {
+  constexpr int NX = Q8 ? D / 64 : D / 32;   // 16-byte loads of a key row per lane
+  constexpr int P = D + 8, NU = 16 * NR * D / 8 / kThreads;
+  __shared__ __attribute__((aligned(16))) bf16_t Qs[16 * NR * P];
+  __shared__ float lam[16 * NR];
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const size_t bh = blockIdx.y;
+  const int b = (int)blockIdx.y / a.Hkv, h = (int)blockIdx.y % a.Hkv;
+  const int32_t* path = PATH ? p.path + (size_t)b * p.A : nullptr;
+  if (PATH && (int)blockIdx.x >= nb) {
+    copy_path<D>(a, p, bh, path, ((int)blockIdx.x - nb) * kThreads + tid);
+    return;
+  }
+  const int ngroups = (a.M + 31) / 32, nwaves = 4 * nb, w0 = 4 * (int)blockIdx.x + wave;
+  u32x4 kr[2][2][NX];
+  float ks[2];
+  // K and the scales of head bh as buffer resources: rows past the cache read as zero
+  constexpr uint32_t kRow = Q8 ? D : 2 * D;   // bytes
+  const __amdgpu_buffer_rsrc_t krs =
+      buffer_rsrc((const char*)a.kc + bh * a.M * (size_t)kRow, (uint32_t)a.M * kRow);
+  const __amdgpu_buffer_rsrc_t srs =
+      buffer_rsrc(Q8 ? a.ks + bh * (size_t)a.M : nullptr, Q8 ? (uint32_t)a.M * 4u : 0u);
+  auto issue = [&](int g, int u) H2O_INLINE {
+    const uint32_t j0 = 32u * (uint32_t)g;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int x = 0; x < NX; ++x)
+        kr[u][kb][x] = __builtin_bit_cast(
+            u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                       krs, (int)((j0 + 16 * kb + l16) * kRow +
+                                  (Q8 ? 16 * g4 + 64 * x
+                                      : 2 * (16 * g4 + 64 * (x >> 1) + 8 * (x & 1)))), 0, 0));
+    if (Q8)
+      ks[u] = __uint_as_float(
+          __builtin_amdgcn_raw_buffer_load_b32(srs, (int)((j0 + (lane & 31)) * 4u), 0, 0));
+  };
+  {
+    // rows of this thread's units, then its row's lambda (a row that is none: +inf,
+    // weights 0), then the first keys, all before anything is used
+    u32x4 qr[NU];
+#pragma unroll
+    for (int e = 0; e < NU; ++e) {
+      const int r = min(tid / (D / 8) + e * (kThreads / (D / 8)), p.R - 1);
+      const int node = max(path_node(path, r / a.G, a.T), 0);
+      qr[e] = *reinterpret_cast<const u32x4*>(
+          a.q + ((size_t)(b * a.Hq + h * a.G + r % a.G) * a.T + node) * D + 8 * (tid % (D / 8)));
+    }
+    float lr = INFINITY;
+    if (tid < p.R) {
+      const int node = path_node(path, tid / a.G, a.T);
+      if (node >= 0) lr = p.lse[(size_t)(b * a.Hq + h * a.G + tid % a.G) * a.T + node] * kLog2e;
+    }
+    issue(w0, 0);
+#pragma unroll
+    for (int e = 0; e < NU; ++e)
+      *reinterpret_cast<u32x4*>(&Qs[(tid / (D / 8) + e * (kThreads / (D / 8))) * P +
+                                    8 * (tid % (D / 8))]) = qr[e];
+    if (tid < 16 * NR) lam[tid] = lr;
+    __syncthreads();
+  }
+  float* dst = p.dst + bh * (size_t)(a.M + p.A);
+  // 32 keys from key j0 on, kf their operands, ck their factors; chunk: key columns of
+  // the chunk, hidden from the rows before them. keep(j): whether column j is a token.
+  auto columns = [&](auto chunk, const bf16x8 (&kf)[2][D / 32], const f32x4 (&ck)[2], int j0,
+                     int nkeys, float* to, auto&& keep) H2O_INLINE {
+    f32x4 s[NR][2], cs[2];
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) s[n][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        const bf16x8 qf = *reinterpret_cast<const bf16x8*>(
+            &Qs[(16 * n + l16) * P + 64 * (x >> 1) + 16 * g4 + 8 * (x & 1)]);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) s[n][kb] = mma(kf[kb][x], qf, s[n][kb]);
+      }
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) cs[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      const float la = lam[16 * n + l16];
+      const int i = decltype(chunk)::value ? (16 * n + l16) / a.G : 0;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float w = __builtin_amdgcn_exp2f(fmaf(s[n][kb][r], ck[kb][r], -la));
+          if (decltype(chunk)::value && j0 + 16 * kb + 4 * g4 + r > i) w = 0.f;
+          cs[kb][r] += w;
+        }
+    }
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float v = cs[kb][r];
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) v += __shfl_xor(v, o, 64);
+        const int j = j0 + 16 * kb + 4 * g4 + r;
+        if (l16 == r && j < nkeys) to[j] = keep(j) ? v : 0.f;
+      }
+  };
+  auto consume = [&](int g, int u) H2O_INLINE {
+    bf16x8 kf[2][D / 32];
+    f32x4 ck[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int x = 0; x < NX; ++x) {
+        const u32x4 v = kr[u][kb][x];
+        if constexpr (Q8) {
+          kf[kb][2 * x] = q8::codes_bf16(v[0], v[1]);
+          kf[kb][2 * x + 1] = q8::codes_bf16(v[2], v[3]);
+        } else {
+          kf[kb][x] = __builtin_bit_cast(bf16x8, v);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        ck[kb][r] = Q8 ? a.c * __shfl(ks[u], 16 * kb + 4 * g4 + r, 64) : a.c;
+    }
+    columns(IntConst<0>{}, kf, ck, 32 * g, a.M, dst, [](int) { return true; });
+  };
+  // whole trips of two groups (one past the cache reads zeros and stores nothing): an
+  // exit or a branch between the two makes the compiler wait for the loads in flight
+  if (nwaves >= ngroups) {
+    if (w0 < ngroups) consume(w0, 0);
+  } else {
+    for (int g = w0; g < ngroups; g += 2 * nwaves) {
+      issue(g + nwaves, 1);
+      __builtin_amdgcn_sched_barrier(0);
+      consume(g, 0);
+      issue(g + 2 * nwaves, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      consume(g + nwaves, 1);
+    }
+  }
+  for (int j0 = 32 * w0; j0 < p.A; j0 += 32 * nwaves) {
+    bf16x8 kf[2][D / 32];
+    f32x4 ck[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      const int i = min(j0 + 16 * kb + l16, p.A - 1);
+      const size_t row = bh * (size_t)a.T + max(path_node(path, i, a.T), 0);
+      ck[kb] = f32x4{a.c, a.c, a.c, a.c};
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x)
+        kf[kb][x] = *reinterpret_cast<const bf16x8*>(a.kn + row * D + 16 * g4 + 64 * (x >> 1) +
+                                                     8 * (x & 1));
+    }
+    columns(IntConst<1>{}, kf, ck, j0, p.A, dst + a.M,
+            [&](int j) { return path_node(path, j, a.T) >= 0; });
+  }
 }
 
 // wsum = the row ranges' sums, in their order.
@@ -877,11 +1051,35 @@ hipError_t launch_columns(const FlashShape& s, const FlashPlan& p, const FlashIn
                           float* wsum, char* ws, float scale, hipStream_t st) {
   const Args a = make_args(s, in, ws, p, scale);
   float* parts = reinterpret_cast<float*>(ws + p.off_parts);
-  const int ncol = path ? A : s.T, nw = column_waves(s, ncol);
+  const int ncol = path ? A : s.T;
+  if (s.G() * ncol <= kFewRows) {
+    const ColArgs c{lse, path, ncol, s.G() * ncol, wsum, (bf16_t*)k_acc, (bf16_t*)v_acc};
+    // blocks per head: as many as are resident (4 per CU, 3 with 64 rows), then as many
+    // as give every wave one group of keys or an even count
+    const int groups = (s.M + 31) / 32, most = (c.R <= 32 ? 4 : 3) * device_cus() / s.BH();
+    int per = most < 1 ? groups : (groups + 4 * most - 1) / (4 * most);
+    if (per > 1) per += per & 1;
+    if (per < 1) per = 1;
+    const int nb = groups ? (groups + 4 * per - 1) / (4 * per) : 1;
+    const dim3 grid(nb + (path ? (A * (s.d / 8) + kThreads - 1) / kThreads : 0), s.BH());
+    return with_cache(s.d, in.q8, [&](auto D, auto q) {
+      constexpr int kD = decltype(D)::value;
+      constexpr bool kQ = decltype(q)::value;
+      auto go = [&](auto kern) {
+        return launch_kernel(K_COLUMNS, kern, grid, dim3(kThreads), st, a, c, nb);
+      };
+      const bool two = c.R <= 32;
+      if (path) return two ? go(column_few<kD, kQ, true, 2>) : go(column_few<kD, kQ, true, 4>);
+      if constexpr (kQ)
+        return two ? go(column_few<kD, true, false, 2>) : go(column_few<kD, true, false, 4>);
+      return hipErrorInvalidValue;
+    });
+  }
+  const int nw = column_waves(s, ncol);
   const int kb = 32 * nw, nt = 64 * nw, tiles = (s.M + kb - 1) / kb + (ncol + kb - 1) / kb;
   const int ncopy = path ? (A * (s.d / 8) + nt - 1) / nt : 0;
   const ColArgs c{lse, path, ncol, s.G() * ncol, p.nranges > 1 ? parts : wsum, (bf16_t*)k_acc,
-                  (bf16_t*)v_acc, ncopy};
+                  (bf16_t*)v_acc};
   const dim3 grid(tiles + ncopy, s.BH(), p.nranges);
   const hipError_t e = with_cache(s.d, in.q8, [&](auto D, auto q) {
     constexpr int kD = decltype(D)::value;
