@@ -74,8 +74,8 @@ __device__ __forceinline__ BlockId block_id(int nsplit) {
 // thread t being t + u * NT.
 template <int D, int NT>
 struct Regs {
-  static constexpr int N16 = BN * D / 8 / NT;
-  static constexpr int N8 = (BN * D / 16 + NT - 1) / NT;   // (8 waves, D = 64: half the threads)
+  static constexpr int N16 = (BN * D / 8 + NT - 1) / NT;   // (8 waves, D = 64: a part of the
+  static constexpr int N8 = (BN * D / 16 + NT - 1) / NT;   // threads; the others load a row again)
   u32x4 k[N16], v[N16];
   float s;                      // thread t < BN: scale of key t; BN <= t < 2 BN: of value t - BN
 };
@@ -103,6 +103,7 @@ __device__ __forceinline__ void store_rows16(bf16_t* lds, const u32x4* r) {
 #pragma unroll
   for (int e = 0; e < Regs<D, NT>::N16; ++e) {
     const int u = threadIdx.x + e * NT;
+    if (BN * D / 8 < NT && u >= BN * D / 8) return;
     *reinterpret_cast<u32x4*>(lds + u / (D / 8) * lds_pitch(D) + 8 * (u % (D / 8))) = r[e];
   }
 }

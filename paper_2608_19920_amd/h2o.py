@@ -162,12 +162,14 @@ def _dev(t: Optional[torch.Tensor], name: str):
 # The current stream's handle without building a torch.cuda.Stream around it
 # (1.5 us a call), where this torch has the accessor.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+# Number of the current device without torch.cuda's own checks (0.5 us a call).
+_device_number = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
         if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
+            return _raw_stream(_device_number())
         return torch.cuda.current_stream().cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
@@ -507,6 +509,27 @@ def h2o_kv_scatter(cache, idx, src, stream=None) -> None:
                                 B, Hkv, M, k, d, _dtype_code(cache), _stream(stream)))
 
 
+def _devs(*named) -> list:
+    """Device pointers of (tensor, name) pairs, None for None: contiguous tensors on the
+    current device, whose stream the call uses."""
+    here, ptrs = None, []
+    for t, name in named:
+        if t is None:
+            ptrs.append(None)
+            continue
+        d = t.get_device()
+        if d != here:
+            if d < 0:
+                raise ValueError(f"{name} must be a device tensor")
+            here = _device_number()
+            if d != here:
+                raise ValueError(f"{name} is on device {d}, the current device is {here}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        ptrs.append(t.data_ptr())
+    return ptrs
+
+
 # ------------------------------------------------- the cache in 8 bits
 def _q8_cache(k_codes, k_scales, v_codes, v_scales):
     """(B, Hkv, M, d) of an 8-bit cache."""
@@ -519,11 +542,6 @@ def _q8_cache(k_codes, k_scales, v_codes, v_scales):
         if t.shape != (B, Hkv, M) or t.dtype != torch.float32:
             raise ValueError(f"{name} must be float32 [B,Hkv,M]")
     return B, Hkv, M, d
-
-
-def _q8_ptrs(k_codes, k_scales, v_codes, v_scales):
-    return (_dev(k_codes, "k_codes"), _dev(k_scales, "k_scales"), _dev(v_codes, "v_codes"),
-            _dev(v_scales, "v_scales"))
 
 
 def _q8_rows(k_rows, v_rows, idx, B, Hkv, M, d):
@@ -543,9 +561,9 @@ def h2o_kv_quantize(k_src, v_src, k_codes, k_scales, v_codes, v_scales, idx=None
     B, Hkv, M, d = _q8_cache(k_codes, k_scales, v_codes, v_scales)
     k = _q8_rows(k_src, v_src, idx, B, Hkv, M, d)
     _check(lib().h2o_kv_quantize(
-        _dev(k_src, "k_src"), _dev(v_src, "v_src"), _dev(idx, "idx"),
-        *_q8_ptrs(k_codes, k_scales, v_codes, v_scales), B, Hkv, M, k, d, _dtype_code(k_src),
-        _stream(stream)))
+        *_devs((k_src, "k_src"), (v_src, "v_src"), (idx, "idx"), (k_codes, "k_codes"),
+               (k_scales, "k_scales"), (v_codes, "v_codes"), (v_scales, "v_scales")),
+        B, Hkv, M, k, d, _dtype_code(k_src), _stream(stream)))
 
 
 def h2o_kv_dequantize(k_codes, k_scales, v_codes, v_scales, k_dst, v_dst, idx=None,
@@ -555,8 +573,9 @@ def h2o_kv_dequantize(k_codes, k_scales, v_codes, v_scales, k_dst, v_dst, idx=No
     B, Hkv, M, d = _q8_cache(k_codes, k_scales, v_codes, v_scales)
     k = _q8_rows(k_dst, v_dst, idx, B, Hkv, M, d)
     _check(lib().h2o_kv_dequantize(
-        *_q8_ptrs(k_codes, k_scales, v_codes, v_scales), _dev(idx, "idx"), _dev(k_dst, "k_dst"),
-        _dev(v_dst, "v_dst"), B, Hkv, M, k, d, _dtype_code(k_dst), _stream(stream)))
+        *_devs((k_codes, "k_codes"), (k_scales, "k_scales"), (v_codes, "v_codes"),
+               (v_scales, "v_scales"), (idx, "idx"), (k_dst, "k_dst"), (v_dst, "v_dst")),
+        B, Hkv, M, k, d, _dtype_code(k_dst), _stream(stream)))
 
 
 def h2o_q8_workspace_bytes(B, Hq, Hkv, T, M, d, dtype, policy="h2o") -> int:
@@ -595,10 +614,10 @@ def h2o_sdpa_chunk_q8(q, k_codes, k_scales, v_codes, v_scales, k_new, v_new, out
     if scale is None:
         scale = sizes[-1] ** -0.5
     _check(lib().h2o_sdpa_chunk_q8(
-        _dev(q, "q"), *_q8_ptrs(k_codes, k_scales, v_codes, v_scales), _dev(k_new, "k_new"),
-        _dev(v_new, "v_new"), _dev(out, "out"), _dev(lse, "lse"), _dev(wsum, "wsum"),
-        _dev(workspace, "workspace"), _nbytes(workspace), *sizes, float(scale), _dtype_code(q),
-        _stream(stream)))
+        *_devs((q, "q"), (k_codes, "k_codes"), (k_scales, "k_scales"), (v_codes, "v_codes"),
+               (v_scales, "v_scales"), (k_new, "k_new"), (v_new, "v_new"), (out, "out"),
+               (lse, "lse"), (wsum, "wsum"), (workspace, "workspace")),
+        _nbytes(workspace), *sizes, float(scale), _dtype_code(q), _stream(stream)))
 
 
 def _evict_q8(scores, token_pos, evict_idx, B, Hkv, M, k):
@@ -621,11 +640,12 @@ def h2o_evict_insert_q8(k_codes, k_scales, v_codes, v_scales, scores, token_pos,
     _evict_q8(scores, token_pos, evict_idx, B, Hkv, M, T)
     if wsum.shape != (B, Hkv, M + T) or wsum.dtype != torch.float32:
         raise ValueError("wsum must be float32 [B,Hkv,M+T]")
+    *ptrs, ws = _devs((k_codes, "k_codes"), (k_scales, "k_scales"), (v_codes, "v_codes"),
+                      (v_scales, "v_scales"), (scores, "scores"), (token_pos, "token_pos"),
+                      (k_new, "k_new"), (v_new, "v_new"), (wsum, "wsum"),
+                      (evict_idx, "evict_idx"), (workspace, "workspace"))
     _check(lib().h2o_evict_insert_q8(
-        *_q8_ptrs(k_codes, k_scales, v_codes, v_scales), _dev(scores, "scores"),
-        _dev(token_pos, "token_pos"), _dev(k_new, "k_new"), _dev(v_new, "v_new"),
-        _dev(wsum, "wsum"), _dev(evict_idx, "evict_idx"), B, Hkv, M, T, d, T, int(pos0),
-        _dtype_code(k_new), _policy_code(policy), _dev(workspace, "workspace"),
+        *ptrs, B, Hkv, M, T, d, T, int(pos0), _dtype_code(k_new), _policy_code(policy), ws,
         _nbytes(workspace), _stream(stream)))
 
 
@@ -640,11 +660,12 @@ def h2o_chunk_step_q8(q, k_codes, k_scales, v_codes, v_scales, scores, token_pos
     if scale is None:
         scale = d ** -0.5
     _check(lib().h2o_chunk_step_q8(
-        _dev(q, "q"), *_q8_ptrs(k_codes, k_scales, v_codes, v_scales), _dev(scores, "scores"),
-        _dev(token_pos, "token_pos"), _dev(k_new, "k_new"), _dev(v_new, "v_new"),
-        _dev(out, "out"), _dev(lse, "lse"), _dev(wsum, "wsum"), _dev(evict_idx, "evict_idx"),
-        _dev(workspace, "workspace"), _nbytes(workspace), *sizes, float(scale), int(pos0),
-        _dtype_code(q), _policy_code(policy), _stream(stream)))
+        *_devs((q, "q"), (k_codes, "k_codes"), (k_scales, "k_scales"), (v_codes, "v_codes"),
+               (v_scales, "v_scales"), (scores, "scores"), (token_pos, "token_pos"),
+               (k_new, "k_new"), (v_new, "v_new"), (out, "out"), (lse, "lse"), (wsum, "wsum"),
+               (evict_idx, "evict_idx"), (workspace, "workspace")),
+        _nbytes(workspace), *sizes, float(scale), int(pos0), _dtype_code(q),
+        _policy_code(policy), _stream(stream)))
 
 
 # ----------------------------------------------- a tree of drafted tokens
@@ -692,11 +713,11 @@ def h2o_sdpa_tree(q, k_cache, v_cache, k_new, v_new, parents, out, lse, workspac
     if scale is None:
         scale = d ** -0.5
     _check(lib().h2o_sdpa_tree(
-        _dev(q, "q"), _dev(k_cache, "k_cache"), _dev(k_scales, "k_scales"),
-        _dev(v_cache, "v_cache"), _dev(v_scales, "v_scales"), _dev(k_new, "k_new"),
-        _dev(v_new, "v_new"), _dev(parents, "parents"), _dev(out, "out"), _dev(lse, "lse"),
-        _dev(workspace, "workspace"), _nbytes(workspace), B, Hq, Hkv, T, M, d, float(scale),
-        _dtype_code(q), _stream(stream)))
+        *_devs((q, "q"), (k_cache, "k_cache"), (k_scales, "k_scales"), (v_cache, "v_cache"),
+               (v_scales, "v_scales"), (k_new, "k_new"), (v_new, "v_new"),
+               (parents, "parents"), (out, "out"), (lse, "lse"), (workspace, "workspace")),
+        _nbytes(workspace), B, Hq, Hkv, T, M, d, float(scale), _dtype_code(q),
+        _stream(stream)))
 
 
 def h2o_tree_accept(q, k_cache, k_new, v_new, lse, path, k_acc, v_acc, wsum, workspace,
@@ -718,9 +739,9 @@ def h2o_tree_accept(q, k_cache, k_new, v_new, lse, path, k_acc, v_acc, wsum, wor
     if scale is None:
         scale = d ** -0.5
     _check(lib().h2o_tree_accept(
-        _dev(q, "q"), _dev(k_cache, "k_cache"), _dev(k_scales, "k_scales"), _dev(k_new, "k_new"),
-        _dev(v_new, "v_new"), _dev(lse, "lse"), _dev(path, "path"), _dev(k_acc, "k_acc"),
-        _dev(v_acc, "v_acc"), _dev(wsum, "wsum"), _dev(workspace, "workspace"),
+        *_devs((q, "q"), (k_cache, "k_cache"), (k_scales, "k_scales"), (k_new, "k_new"),
+               (v_new, "v_new"), (lse, "lse"), (path, "path"), (k_acc, "k_acc"),
+               (v_acc, "v_acc"), (wsum, "wsum"), (workspace, "workspace")),
         _nbytes(workspace), B, Hq, Hkv, T, M, A, d, float(scale), _dtype_code(q),
         _stream(stream)))
 

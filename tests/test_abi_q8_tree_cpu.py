@@ -192,3 +192,29 @@ def test_binding_checks_shapes_and_types():
                           z(1, 2, 18), ws, k_scales=sc)
     with pytest.raises(ValueError):      # host tensors
         H.h2o_kv_quantize(rows, rows, k8, sc, k8, sc)
+
+
+class _Elsewhere:
+    """A stand-in for a contiguous tensor on a device (-1: the host)."""
+
+    def __init__(self, device, contiguous=True):
+        self.device, self.contiguous = device, contiguous
+
+    def get_device(self):
+        return self.device
+
+    def is_contiguous(self):
+        return self.contiguous
+
+    def data_ptr(self):
+        return 16 + self.device
+
+
+def test_binding_refuses_other_devices_and_strides(monkeypatch):
+    monkeypatch.setattr(H, "_device_number", lambda: 1)
+    assert H._devs((_Elsewhere(1), "a"), (None, "b"), (_Elsewhere(1), "c")) == [17, None, 17]
+    for bad, what in (((_Elsewhere(1), _Elsewhere(0)), "device 0"), ((_Elsewhere(2),), "device 2"),
+                      ((_Elsewhere(-1),), "device tensor"), ((_Elsewhere(1), _Elsewhere(-1)), "device tensor"),
+                      ((_Elsewhere(1, False),), "contiguous")):
+        with pytest.raises(ValueError, match=what):
+            H._devs(*((t, "x") for t in bad))
