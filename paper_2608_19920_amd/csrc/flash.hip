@@ -28,7 +28,6 @@ namespace {
 
 using namespace mfma;
 
-constexpr int BN = 32;          // keys per tile
 constexpr int kThreads = 256;
 constexpr int kXcds = 8;
 constexpr int kWaveTree = 64;   // nodes of a tree that a wave masks by itself
@@ -72,7 +71,7 @@ __device__ __forceinline__ BlockId block_id(int nsplit) {
 // ------------------------------------------------------------------- staging
 // A tile's rows in registers: 16-byte units, 16 codes or 8 bf16 each, unit u of
 // thread t being t + u * NT.
-template <int D, int NT>
+template <int D, int NT, int BN>
 struct Regs {
   static constexpr int N16 = (BN * D / 8 + NT - 1) / NT;   // (8 waves, D = 64: a part of the
   static constexpr int N8 = (BN * D / 16 + NT - 1) / NT;   // threads; the others load a row again)
@@ -80,37 +79,37 @@ struct Regs {
   float s;                      // thread t < BN: scale of key t; BN <= t < 2 BN: of value t - BN
 };
 
-template <int D, int NT>
+template <int D, int NT, int BN>
 __device__ __forceinline__ void load_rows16(u32x4* r, const void* base, int n) {
   const char* p = reinterpret_cast<const char*>(base);
 #pragma unroll
-  for (int e = 0; e < Regs<D, NT>::N16; ++e) {
+  for (int e = 0; e < Regs<D, NT, BN>::N16; ++e) {
     const int u = threadIdx.x + e * NT, row = min(u / (D / 8), n - 1);
     r[e] = *reinterpret_cast<const u32x4*>(p + (uint32_t)(row * D + 8 * (u % (D / 8))) * 2u);
   }
 }
-template <int D, int NT>
+template <int D, int NT, int BN>
 __device__ __forceinline__ void load_rows8(u32x4* r, const void* base, int n) {
   const char* p = reinterpret_cast<const char*>(base);
 #pragma unroll
-  for (int e = 0; e < Regs<D, NT>::N8; ++e) {
+  for (int e = 0; e < Regs<D, NT, BN>::N8; ++e) {
     const int u = threadIdx.x + e * NT, row = min(u / (D / 16), n - 1);
     r[e] = *reinterpret_cast<const u32x4*>(p + (uint32_t)(row * D + 16 * (u % (D / 16))));
   }
 }
-template <int D, int NT>
+template <int D, int NT, int BN>
 __device__ __forceinline__ void store_rows16(bf16_t* lds, const u32x4* r) {
 #pragma unroll
-  for (int e = 0; e < Regs<D, NT>::N16; ++e) {
+  for (int e = 0; e < Regs<D, NT, BN>::N16; ++e) {
     const int u = threadIdx.x + e * NT;
     if (BN * D / 8 < NT && u >= BN * D / 8) return;
     *reinterpret_cast<u32x4*>(lds + u / (D / 8) * lds_pitch(D) + 8 * (u % (D / 8))) = r[e];
   }
 }
-template <int D, int NT>
+template <int D, int NT, int BN>
 __device__ __forceinline__ void store_rows8(bf16_t* lds, const u32x4* r) {
 #pragma unroll
-  for (int e = 0; e < Regs<D, NT>::N8; ++e) {
+  for (int e = 0; e < Regs<D, NT, BN>::N8; ++e) {
     const int u = threadIdx.x + e * NT;
     if (BN * D / 16 < NT && u >= BN * D / 16) return;
     bf16x8* dst = reinterpret_cast<bf16x8*>(lds + u / (D / 16) * lds_pitch(D) + 16 * (u % (D / 16)));
@@ -121,37 +120,37 @@ __device__ __forceinline__ void store_rows8(bf16_t* lds, const u32x4* r) {
 
 // Rows past the tile's end re-read its last row (in bounds; masked later).
 // WHOLE: the caller knows that it is a whole cache tile (no branch).
-template <int D, bool Q8, int NT, bool WHOLE = false>
-__device__ __forceinline__ void load_tile(Regs<D, NT>& g, const Args& a, size_t bh, int t, int tc) {
+template <int D, bool Q8, int NT, int BN, bool WHOLE = false>
+__device__ __forceinline__ void load_tile(Regs<D, NT, BN>& g, const Args& a, size_t bh, int t, int tc) {
   if (WHOLE || t < tc) {
     const int j0 = t * BN, n = WHOLE ? BN : min(BN, a.M - j0);
     const size_t row = bh * (size_t)a.M + j0;
     if constexpr (Q8) {
-      load_rows8<D, NT>(g.k, (const int8_t*)a.kc + row * D, n);
-      load_rows8<D, NT>(g.v, (const int8_t*)a.vc + row * D, n);
+      load_rows8<D, NT, BN>(g.k, (const int8_t*)a.kc + row * D, n);
+      load_rows8<D, NT, BN>(g.v, (const int8_t*)a.vc + row * D, n);
       const int r = threadIdx.x % BN;
       if (threadIdx.x < 2 * BN) g.s = (threadIdx.x < BN ? a.ks : a.vs)[row + min(r, n - 1)];
     } else {
-      load_rows16<D, NT>(g.k, (const bf16_t*)a.kc + row * D, n);
-      load_rows16<D, NT>(g.v, (const bf16_t*)a.vc + row * D, n);
+      load_rows16<D, NT, BN>(g.k, (const bf16_t*)a.kc + row * D, n);
+      load_rows16<D, NT, BN>(g.v, (const bf16_t*)a.vc + row * D, n);
     }
   } else {
     const int j0 = (t - tc) * BN, n = min(BN, a.T - j0);
     const size_t row = bh * (size_t)a.T + j0;
-    load_rows16<D, NT>(g.k, a.kn + row * D, n);
-    load_rows16<D, NT>(g.v, a.vn + row * D, n);
+    load_rows16<D, NT, BN>(g.k, a.kn + row * D, n);
+    load_rows16<D, NT, BN>(g.v, a.vn + row * D, n);
     if (Q8) g.s = 1.f;
   }
 }
-template <int D, bool Q8, int NT, bool WHOLE = false>
+template <int D, bool Q8, int NT, int BN, bool WHOLE = false>
 __device__ __forceinline__ void store_tile(bf16_t* Ks, bf16_t* Vs, float* sc,
-                                           const Regs<D, NT>& g, const Args& a, int t, int tc) {
+                                           const Regs<D, NT, BN>& g, const Args& a, int t, int tc) {
   if (Q8 && (WHOLE || t < tc)) {
-    store_rows8<D, NT>(Ks, g.k);
-    store_rows8<D, NT>(Vs, g.v);
+    store_rows8<D, NT, BN>(Ks, g.k);
+    store_rows8<D, NT, BN>(Vs, g.v);
   } else {
-    store_rows16<D, NT>(Ks, g.k);
-    store_rows16<D, NT>(Vs, g.v);
+    store_rows16<D, NT, BN>(Ks, g.k);
+    store_rows16<D, NT, BN>(Vs, g.v);
   }
   if (Q8 && threadIdx.x < 2 * BN) sc[threadIdx.x] = threadIdx.x < BN ? g.s * a.c : g.s;
 }
@@ -164,6 +163,11 @@ __device__ __forceinline__ void store_tile(bf16_t* Ks, bf16_t* Vs, float* sc,
 // wave-uniform and rare branch), so terms stay below 2^64, far inside float32 and
 // bf16.
 //
+// Tiles have BN keys, 32, or 64 at d = 64 with 128 rows or more, where the registers
+// allow them: half the barriers, and more of a wave's own products and exponentials to
+// overlap (B1 Hq32 Hkv8 d64 M8192 T1024 128 -> 120 us; at d = 128 they spill, with 64
+// rows B4 Hkv8 d64 M8192, a tree of 16, 17.5 -> 23.3).
+//
 // Tile t + 2 is on its way from memory to registers and tile t + 1 from registers to
 // the other LDS buffer while tile t is used; one barrier a tile. (Multiplying the
 // scores of tile t + 1 during the exponentials of tile t, a third buffer, requests
@@ -174,13 +178,13 @@ __device__ __forceinline__ void store_tile(bf16_t* Ks, bf16_t* Vs, float* sc,
 // vector operations, 16 of them exponentials (8 cycles), per 32 keys and 32 rows; 64
 // of the 190 turn codes into bf16. With 8 waves a block they are half as many per row:
 // 191 us at the shape above, 765 TFLOP/s on the visible pairs.
-template <int D, bool Q8, bool TREE, int NQB, int NW>
+template <int D, bool Q8, bool TREE, int NQB, int NW, int BN>
 __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
                                                          bf16_t* __restrict__ out,
                                                          float* __restrict__ lse,
                                                          float2* __restrict__ stats,
                                                          float* __restrict__ opart) {
-  constexpr int NT = NW * 64, ROWS = NW * NQB * 16, P = lds_pitch(D);
+  constexpr int NT = NW * 64, ROWS = NW * NQB * 16, P = lds_pitch(D), NK = BN / 16;
   __shared__ __attribute__((aligned(16))) bf16_t Ks[2][BN * P];
   __shared__ __attribute__((aligned(16))) bf16_t Vs[2][BN * P];
   __shared__ __attribute__((aligned(16))) float sc[2][2 * BN];
@@ -240,12 +244,12 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
   // Tile t, in LDS at K, V, scl: scores, probabilities, O += P V; then the registers g,
   // with tile t + 1, go to the other buffer, and tile t + 2 is requested into them.
   auto tile = [&](auto masked, auto whole, int t, const bf16_t* K, const bf16_t* V,
-                  const float* scl, Regs<D, NT>& g, int t1st, int t2nd, bf16_t* K2, bf16_t* V2,
+                  const float* scl, Regs<D, NT, BN>& g, int t1st, int t2nd, bf16_t* K2, bf16_t* V2,
                   float* scl2) H2O_INLINE {
     constexpr bool MASK = decltype(masked)::value, WHOLE = decltype(whole)::value;
-    f32x4 s[2][NQB];
+    f32x4 s[NK][NQB];
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
+    for (int kb = 0; kb < NK; ++kb) {
 #pragma unroll
       for (int n = 0; n < NQB; ++n) s[kb][n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -256,41 +260,47 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
       }
     }
     const bool cache = t < tc;
-    uint32_t seen[NQB];
+    uint32_t seen[NQB][BN / 32];
     if (MASK && TREE && !cache)
 #pragma unroll
       for (int n = 0; n < NQB; ++n)
-        seen[n] = a.T <= kWaveTree ? (uint32_t)(own[n] >> (t > tc ? 32 : 0))
-                                   : a.bits[((size_t)b * a.T + qi[n]) * a.W + (t - tc)];
-    f32x4 cks[2], cvs[2];
+#pragma unroll
+        for (int w = 0; w < BN / 32; ++w) {
+          const int word = (t - tc) * (BN / 32) + w;
+          seen[n][w] = word >= a.W ? 0u
+                       : a.T <= kWaveTree ? (uint32_t)(own[n] >> (word ? 32 : 0))
+                                          : a.bits[((size_t)b * a.T + qi[n]) * a.W + word];
+        }
+    f32x4 cks[NK], cvs[NK];
     if (Q8)
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
+      for (int kb = 0; kb < NK; ++kb) {
         cks[kb] = *reinterpret_cast<const f32x4*>(scl + 16 * kb + 4 * g4);
         cvs[kb] = *reinterpret_cast<const f32x4*>(scl + BN + 16 * kb + 4 * g4);
       }
-    auto shifted = [&](int n, float ref, float (&x)[8]) H2O_INLINE {
+    auto shifted = [&](int n, float ref, float (&x)[4 * NK]) H2O_INLINE {
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+      for (int kb = 0; kb < NK; ++kb)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           float v = fmaf(s[kb][n][r], Q8 ? cks[kb][r] : a.c, -ref);
           if (MASK) {
             const int j = 16 * kb + 4 * g4 + r;
             const bool hid = cache ? t * BN + j >= a.M
-                             : TREE ? !((seen[n] >> j) & 1u) : (t - tc) * BN + j > qi[n];
+                             : TREE ? !((seen[n][kb >> 1] >> (j & 31)) & 1u) : (t - tc) * BN + j > qi[n];
             if (hid) v = -INFINITY;
           }
           x[4 * kb + r] = v;
         }
     };
-    float x[NQB][8], mx[NQB];
+    float x[NQB][4 * NK], mx[NQB];
     bool up = false;
 #pragma unroll
     for (int n = 0; n < NQB; ++n) {
       shifted(n, mu[n], x[n]);
-      mx[n] = fmaxf(fmaxf(fmaxf(x[n][0], x[n][1]), x[n][2]),
-                    fmaxf(fmaxf(fmaxf(x[n][3], x[n][4]), x[n][5]), fmaxf(x[n][6], x[n][7])));
+      mx[n] = x[n][0];
+#pragma unroll
+      for (int e = 1; e < 4 * NK; ++e) mx[n] = fmaxf(mx[n], x[n][e]);
       up |= mx[n] > thr[n];
     }
     if (__builtin_amdgcn_ballot_w64(up)) {
@@ -308,32 +318,35 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
         shifted(n, mu[n], x[n]);
       }
     }
-    bf16x8 pb[NQB];
 #pragma unroll
-    for (int n = 0; n < NQB; ++n)
+    for (int kk = 0; kk < BN / 32; ++kk) {
+      bf16x8 pb[NQB];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float p = __builtin_amdgcn_exp2f(x[n][e]);
-        l[n] += p;
-        pb[n][e] = (__bf16)(Q8 ? p * cvs[e >> 2][e & 3] : p);
+      for (int n = 0; n < NQB; ++n)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float p = __builtin_amdgcn_exp2f(x[n][8 * kk + e]);
+          l[n] += p;
+          pb[n][e] = (__bf16)(Q8 ? p * cvs[2 * kk + (e >> 2)][e & 3] : p);
+        }
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) {
+        const bf16x8 vf = tr_operand(V + 32 * kk * P, P, db, lane);
+#pragma unroll
+        for (int n = 0; n < NQB; ++n) oacc[db][n] = mma(vf, pb[n], oacc[db][n]);
       }
-#pragma unroll
-    for (int db = 0; db < D / 16; ++db) {
-      const bf16x8 vf = tr_operand(V, P, db, lane);
-#pragma unroll
-      for (int n = 0; n < NQB; ++n) oacc[db][n] = mma(vf, pb[n], oacc[db][n]);
     }
-    store_tile<D, Q8, NT, WHOLE>(K2, V2, scl2, g, a, t1st, tc);
-    load_tile<D, Q8, NT, WHOLE>(g, a, bh, t2nd, tc);
+    store_tile<D, Q8, NT, BN, WHOLE>(K2, V2, scl2, g, a, t1st, tc);
+    load_tile<D, Q8, NT, BN, WHOLE>(g, a, bh, t2nd, tc);
     __syncthreads();
   };
 
   if (t0 < t1) {
-    Regs<D, NT> g;
+    Regs<D, NT, BN> g;
     const int last = t1 - 1;
-    load_tile<D, Q8, NT>(g, a, bh, t0, tc);
-    store_tile<D, Q8, NT>(Ks[0], Vs[0], sc[0], g, a, t0, tc);
-    load_tile<D, Q8, NT>(g, a, bh, min(t0 + 1, last), tc);
+    load_tile<D, Q8, NT, BN>(g, a, bh, t0, tc);
+    store_tile<D, Q8, NT, BN>(Ks[0], Vs[0], sc[0], g, a, t0, tc);
+    load_tile<D, Q8, NT, BN>(g, a, bh, min(t0 + 1, last), tc);
     __syncthreads();
     auto run = [&](auto masked, auto whole, int ta, int tb) H2O_INLINE {
       for (int t = ta; t < tb; ++t) {
@@ -910,16 +923,16 @@ Args make_args(const FlashShape& s, const FlashIn& in, const char* ws, const Fla
 // start and end; the partials of several ranges are written, read and merged (3 us
 // and a byte of them in 1 / 3 TB/s). At B1 Hkv8 G4 T1024 d128 the plan takes 256 rows
 // and two ranges, 193 + 8 us; 128 rows 221 + 8, four ranges 206 + 13. At d64 256 rows
-// and two ranges 140 + 5, 128 rows and three 145 + 6. At T256 d128 64 rows and four
+// and two ranges 144 + 5, 128 rows and three 141 + 6. At T256 d128 64 rows and four
 // ranges 75 + 4 us, two 98 + 4.
 FlashPlan flash_plan(const FlashShape& s, bool tree) {
   FlashPlan p{};
   const long long BH = s.BH(), R = (long long)s.G() * s.T, cus = device_cus();
-  const long long ntiles = (s.M + BN - 1) / BN + (s.T + BN - 1) / BN;
+  const long long ntiles = (s.M + 31) / 32 + (s.T + 31) / 32;
   struct Block { int rows, resident; double us[4]; };
   static const Block k128[] = {{64, 3, {0.75, 1.13, 1.57}}, {128, 2, {1.05, 1.6}}, {256, 1, {1.4}}};
   static const Block k64[] = {{64, 4, {0.62, 0.87, 1.11, 1.41}}, {128, 3, {0.86, 1.21, 1.58}},
-                              {256, 1, {1.02}}};
+                              {256, 1, {1.06}}};
   // float32: 64 rows, two blocks per CU, 16 times the products' time
   static const Block kF32[] = {{64, 2, {4.0, 5.5}}};
   const Block* const blocks = s.f32 ? kF32 : s.d == 64 ? k64 : k128;
@@ -1035,9 +1048,10 @@ hipError_t launch_flash(const FlashShape& s, const FlashPlan& p, const FlashIn& 
     };
     auto rows = [&](auto mask) {
       constexpr bool kT = decltype(mask)::value;
-      return p.rows == 256   ? go(flash_pass<kD, kQ, kT, 2, 8>)
-             : p.rows == 128 ? go(flash_pass<kD, kQ, kT, 2, 4>)
-                             : go(flash_pass<kD, kQ, kT, 1, 4>);
+      constexpr int kBN = kD == 64 ? 64 : 32;
+      return p.rows == 256   ? go(flash_pass<kD, kQ, kT, 2, 8, kBN>)
+             : p.rows == 128 ? go(flash_pass<kD, kQ, kT, 2, 4, kBN>)
+                             : go(flash_pass<kD, kQ, kT, 1, 4, 32>);
     };
     if (tree) return rows(IntConst<1>{});
     if constexpr (kQ) return rows(IntConst<0>{});
