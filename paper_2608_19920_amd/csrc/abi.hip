@@ -1001,42 +1001,60 @@ int check_attend_q8(const void* q, const CacheQ8& c, const void* k_new, const vo
   return H2O_OK;
 }
 
+// The attention with the summed weights. scores non-null: these are added to them, by
+// the column sums where they are a kernel of their own; keys non-null as well: set to a
+// copy of the accumulated scores, or to the scores where there is none.
 hipError_t launch_attend_q8(const void* q, const CacheQ8& c, const void* k_new, const void* v_new,
                             void* out, float* lse, float* wsum, char* ws, int B, int Hq, int Hkv,
-                            int T, int M, int d, float scale, int dtype, hipStream_t st) {
+                            int T, int M, int d, float scale, int dtype, hipStream_t st,
+                            float* scores = nullptr, const float** keys = nullptr) {
   if (token_q8(Hq, Hkv, T, d, dtype)) {
     const Shape s{B, Hq, Hkv, T, M, d};
-    return launch_sdpa_decode_q8(s, path_plan(s, 2), q, c, k_new, v_new, out, lse, wsum, ws, scale,
-                                 st);
+    hipError_t e = launch_sdpa_decode_q8(s, path_plan(s, 2), q, c, k_new, v_new, out, lse, wsum, ws,
+                                         scale, st);
+    if (e == hipSuccess && scores) e = launch_accumulate(scores, wsum, B * Hkv, M, T, st);
+    if (keys) *keys = scores;
+    return e;
   }
   const FlashShape s{B, Hq, Hkv, T, M, d, dtype == H2O_F32};
   const FlashPlan p = flash_plan(s, false);
   const FlashIn in{true, q, c.k, c.v, c.ks, c.vs, k_new, v_new};
+  float* copy = keys ? reinterpret_cast<float*>(ws + p.off_keys) : nullptr;
+  if (keys) *keys = copy;
   hipError_t e = (s.f32 ? launch_flash_f32 : launch_flash)(s, p, in, out, lse, ws, scale, st);
   if (e != hipSuccess) return e;
   return (s.f32 ? launch_columns_f32 : launch_columns)(s, p, in, lse, nullptr, 0, nullptr, nullptr,
-                                                       wsum, ws, scale, st);
+                                                       wsum, ws, scale, st, ScoreAcc{scores, copy});
 }
 
 // The ranking of `policy` against age t, then the chunk's rows in 8 bits, scores
-// and positions into the k slots. ews: scratch of evict_workspace().
-hipError_t launch_evict_q8(int policy, const CacheQ8& c, float* scores, int32_t* token_pos,
-                           const void* k_new, const void* v_new, const float* wsum,
-                           int32_t* evict_idx, int B, int Hkv, int M, int T, int d, int k,
-                           int32_t pos0, int32_t t, bool f32, char* ews, hipStream_t st) {
+// and positions into the k slots. ews: scratch of evict_workspace(); ranked: the scores,
+// or a copy of them, which a selection and insert in one launch needs for more than a
+// few rows.
+hipError_t launch_evict_q8(int policy, const CacheQ8& c, float* scores, const float* ranked,
+                           int32_t* token_pos, const void* k_new, const void* v_new,
+                           const float* wsum, int32_t* evict_idx, int B, int Hkv, int M, int T,
+                           int d, int k, int32_t pos0, int32_t t, bool f32, char* ews,
+                           hipStream_t st) {
   const int rows = B * Hkv;
-  float* keys = reinterpret_cast<float*>(ews);
+  float* wk = reinterpret_cast<float*>(ews);
   hipError_t e = hipSuccess;
   if (policy == H2O_POLICY_ORIG) {
     int32_t* head_idx = reinterpret_cast<int32_t*>(ews + align256((size_t)Hkv * M * 4));
-    e = launch_orig_keys(scores, keys, B, Hkv, M, st);
-    if (e == hipSuccess) e = launch_bottomk(keys, Hkv, M, k, head_idx, st);
+    e = launch_orig_keys(scores, wk, B, Hkv, M, st);
+    if (e == hipSuccess) e = launch_bottomk(wk, Hkv, M, k, head_idx, st);
     if (e == hipSuccess) e = launch_broadcast_rows(head_idx, evict_idx, B, Hkv * k, st);
-  } else if (policy == H2O_POLICY_NORM) {
-    e = launch_norm_keys(scores, token_pos, keys, rows, M, t, st);
-    if (e == hipSuccess) e = launch_bottomk(keys, rows, M, k, evict_idx, st);
   } else {
-    e = launch_bottomk(scores, rows, M, k, evict_idx, st);
+    if (policy == H2O_POLICY_NORM) {
+      e = launch_norm_keys(scores, token_pos, wk, rows, M, t, st);
+      ranked = wk;
+    }
+    if (e != hipSuccess) return e;
+    if (ranked != scores ? bottomk_insert_supported(k)
+                         : bottomk_insert_in_place(M, k, d, f32 ? 4 : 2))
+      return launch_bottomk_insert_q8(ranked, scores, token_pos, c, k_new, v_new, wsum, evict_idx,
+                                      rows, M, T, d, k, pos0, f32, st);
+    e = launch_bottomk(ranked, rows, M, k, evict_idx, st);
   }
   if (e != hipSuccess) return e;
   return launch_kv_quantize(k_new, v_new, evict_idx, c, rows, M, k, d, f32, st, scores, token_pos,
@@ -1140,7 +1158,7 @@ int h2o_evict_insert_q8(int8_t* k_codes, float* k_scales, int8_t* v_codes, float
   if (!aligned16(workspace)) return fail(H2O_EALIGN, "workspace not 16-byte aligned");
   rc = check_device();
   if (rc) return rc;
-  return launched(launch_evict_q8(policy, c, scores, token_pos, k_new, v_new, wsum, evict_idx, B,
+  return launched(launch_evict_q8(policy, c, scores, scores, token_pos, k_new, v_new, wsum, evict_idx, B,
                                   Hkv, M, T, d, k, pos0, pos0 + T, dtype == H2O_F32,
                                   reinterpret_cast<char*>(workspace),
                                   reinterpret_cast<hipStream_t>(stream)));
@@ -1170,12 +1188,13 @@ int h2o_chunk_step_q8(const void* q, int8_t* k_codes, float* k_scales, int8_t* v
     return launched(launch_decode_step_q8(s, path_plan(s, 2), q, c, k_new, v_new, out, lse, wsum,
                                           scores, token_pos, evict_idx, pos0, ws, scale, st));
   }
+  const float* ranked = scores;
+  const bool copy = policy == H2O_POLICY_H2O && bottomk_insert_supported(T);
   hipError_t e = launch_attend_q8(q, c, k_new, v_new, out, lse, wsum, ws, B, Hq, Hkv, T, M, d,
-                                  scale, dtype, st);
-  if (e == hipSuccess) e = launch_accumulate(scores, wsum, B * Hkv, M, T, st);
+                                  scale, dtype, st, scores, copy ? &ranked : nullptr);
   if (e == hipSuccess)
-    e = launch_evict_q8(policy, c, scores, token_pos, k_new, v_new, wsum, evict_idx, B, Hkv, M, T,
-                        d, T, pos0, pos0 + T, dtype == H2O_F32,
+    e = launch_evict_q8(policy, c, scores, ranked, token_pos, k_new, v_new, wsum, evict_idx, B, Hkv,
+                        M, T, d, T, pos0, pos0 + T, dtype == H2O_F32,
                         ws + attend_q8_bytes(B, Hq, Hkv, T, M, d, dtype), st);
   return launched(e);
 }
@@ -1230,7 +1249,7 @@ int h2o_tree_accept(const void* q, const void* k_cache, const float* k_scales, c
   const FlashIn in{k_scales != nullptr, q, k_cache, nullptr, k_scales, nullptr, k_new, v_new};
   return launched((s.f32 ? launch_columns_f32 : launch_columns)(
       s, p, in, lse, path, A, k_acc, v_acc, wsum, reinterpret_cast<char*>(workspace), scale,
-      reinterpret_cast<hipStream_t>(stream)));
+      reinterpret_cast<hipStream_t>(stream), ScoreAcc{}));
 }
 
 }  // extern "C"

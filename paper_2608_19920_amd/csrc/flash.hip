@@ -481,6 +481,7 @@ struct ColArgs {
   int A, R;                     // chunk key columns and packed rows
   float* dst;                   // [ranges of rows][BH][M + A]
   bf16_t *k_acc, *v_acc;        // path: [BH][A][D], the path's keys and values
+  ScoreAcc acc;                 // (one range of rows)
 };
 constexpr int kQRows = 64;      // rows per step
 constexpr int kFewRows = 64;    // rows that a wave keeps (column_few)
@@ -509,7 +510,7 @@ __device__ __forceinline__ void copy_path(const Args& a, const ColArgs& p, size_
 
 template <int D, bool Q8, bool PATH, int NKB, int NW>
 __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void column_pass(Args a, ColArgs p) {
-  constexpr int NT = NW * 64, KB = NW * NKB * 16, P = D + 8, NU = kQRows * D / 8 / NT;
+  constexpr int NT = NW * 64, KB = NW * NKB * 16, P = lds_pitch(D), NU = kQRows * D / 8 / NT;
   __shared__ __attribute__((aligned(16))) bf16_t Qs[2][kQRows * P];
   __shared__ float lam[2][kQRows];
   __shared__ int pos[2][kQRows];
@@ -533,25 +534,26 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void column_pass(Args a, 
   const bool cache = bx < tc;
   const int j0 = (cache ? bx : bx - tc) * KB + wave * NKB * 16;
   const int nkeys = cache ? a.M : p.A;
-  // this lane's operand rows: key j0 + 16 kb + l16, elements 64 x + 16 g4 .. +15
-  // (an order of d that both operands share; 16 codes are one load). All that the
-  // block reads first is requested before any of it is used.
+  // this lane's operand rows: key j0 + 16 kb + l16, elements 32 x + 8 g4 .. +7. All
+  // that the block reads first is requested before any of it is used.
   u32x4 kr[NKB][D / 32];
   f32x4 cks[NKB], cs[NKB];
 #pragma unroll
   for (int kb = 0; kb < NKB; ++kb) {
     const int j = min(j0 + 16 * kb + l16, nkeys - 1);
     if (Q8 && cache) {
-      const int8_t* src = (const int8_t*)a.kc + (bh * a.M + j) * (size_t)D + 16 * g4;
+      const int8_t* src = (const int8_t*)a.kc + (bh * a.M + j) * (size_t)D + 8 * g4;
 #pragma unroll
-      for (int x = 0; x < D / 64; ++x) kr[kb][x] = *reinterpret_cast<const u32x4*>(src + 64 * x);
+      for (int x = 0; x < D / 32; ++x) {
+        const uint2 v = *reinterpret_cast<const uint2*>(src + 32 * x);
+        kr[kb][x] = u32x4{v.x, v.y, 0u, 0u};
+      }
     } else {
       const int n = cache ? j : max(node_of(j), 0);
       const bf16_t* src = (cache ? (const bf16_t*)a.kc + (bh * a.M + n) * (size_t)D
-                                 : a.kn + (bh * a.T + n) * (size_t)D) + 16 * g4;
+                                 : a.kn + (bh * a.T + n) * (size_t)D) + 8 * g4;
 #pragma unroll
-      for (int x = 0; x < D / 32; ++x)
-        kr[kb][x] = *reinterpret_cast<const u32x4*>(src + 64 * (x >> 1) + 8 * (x & 1));
+      for (int x = 0; x < D / 32; ++x) kr[kb][x] = *reinterpret_cast<const u32x4*>(src + 32 * x);
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -618,16 +620,10 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void column_pass(Args a, 
 #pragma unroll
   for (int kb = 0; kb < NKB; ++kb) {
     cks[kb] *= a.c;
-    if (Q8 && cache) {
 #pragma unroll
-      for (int x = 0; x < D / 64; ++x) {
-        kf[kb][2 * x] = q8::codes_bf16(kr[kb][x][0], kr[kb][x][1]);
-        kf[kb][2 * x + 1] = q8::codes_bf16(kr[kb][x][2], kr[kb][x][3]);
-      }
-    } else {
-#pragma unroll
-      for (int x = 0; x < D / 32; ++x) kf[kb][x] = __builtin_bit_cast(bf16x8, kr[kb][x]);
-    }
+    for (int x = 0; x < D / 32; ++x)
+      kf[kb][x] = Q8 && cache ? q8::codes_bf16(kr[kb][x][0], kr[kb][x][1])
+                              : __builtin_bit_cast(bf16x8, kr[kb][x]);
   }
   // the products of the next 16 rows go out before the exponentials of these
   auto step = [&](auto chunk, int buf) H2O_INLINE {
@@ -637,8 +633,7 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void column_pass(Args a, 
       for (int kb = 0; kb < NKB; ++kb) d[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) {
-        const bf16x8 qf = *reinterpret_cast<const bf16x8*>(
-            &Qs[buf][(16 * n + l16) * P + 64 * (x >> 1) + 16 * g4 + 8 * (x & 1)]);
+        const bf16x8 qf = row_operand(Qs[buf], P, 16 * n + l16, 32 * x, lane);
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb) d[kb] = mma(kf[kb][x], qf, d[kb]);
       }
@@ -684,7 +679,10 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void column_pass(Args a, 
 #pragma unroll
       for (int o = 1; o < 16; o <<= 1) v += __shfl_xor(v, o, 64);
       const int j = j0 + 16 * kb + 4 * g4 + r;
-      if (l16 == 0 && j < nkeys) dst[j] = PATH && !cache && node_of(j) < 0 ? 0.f : v;
+      if (l16 == 0 && j < nkeys) {
+        dst[j] = PATH && !cache && node_of(j) < 0 ? 0.f : v;
+        if (cache) p.acc.add(bh * a.M + j, v);
+      }
     }
 }
 
@@ -710,15 +708,23 @@ __global__ __launch_bounds__(kThreads) void column_few(Args a, ColArgs p, int nb
   }
   const int ngroups = (a.M + 31) / 32, nwaves = 4 * nb, w0 = 4 * (int)blockIdx.x + wave;
   u32x4 kr[2][2][NX];
-  float ks[2];
+  float ks[2], old[2][2];       // old: the scores of this lane's columns (lanes l16 < 4)
   // K and the scales of head bh as buffer resources: rows past the cache read as zero
   constexpr uint32_t kRow = Q8 ? D : 2 * D;   // bytes
   const __amdgpu_buffer_rsrc_t krs =
       buffer_rsrc((const char*)a.kc + bh * a.M * (size_t)kRow, (uint32_t)a.M * kRow);
   const __amdgpu_buffer_rsrc_t srs =
       buffer_rsrc(Q8 ? a.ks + bh * (size_t)a.M : nullptr, Q8 ? (uint32_t)a.M * 4u : 0u);
+  // (a score asked for behind the keys of a later group would be waited for with them)
+  const __amdgpu_buffer_rsrc_t ors =
+      buffer_rsrc(p.acc.scores ? p.acc.scores + bh * (size_t)a.M : nullptr,
+                  p.acc.scores ? (uint32_t)a.M * 4u : 0u);
   auto issue = [&](int g, int u) H2O_INLINE {
     const uint32_t j0 = 32u * (uint32_t)g;
+#pragma unroll
+    for (int kb = 0; kb < 2 && !PATH; ++kb)   // (a path's calls add to no scores)
+      old[u][kb] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(
+          ors, (int)(l16 < 4 ? (j0 + 16 * kb + 4 * g4 + l16) * 4u : 0x7FFFFFF0u), 0, 0));
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -760,7 +766,7 @@ __global__ __launch_bounds__(kThreads) void column_few(Args a, ColArgs p, int nb
   // 32 keys from key j0 on, kf their operands, ck their factors; chunk: key columns of
   // the chunk, hidden from the rows before them. keep(j): whether column j is a token.
   auto columns = [&](auto chunk, const bf16x8 (&kf)[2][D / 32], const f32x4 (&ck)[2], int j0,
-                     int nkeys, float* to, auto&& keep) H2O_INLINE {
+                     int nkeys, float* to, const float (&prior)[2], auto&& keep) H2O_INLINE {
     f32x4 s[NR][2], cs[2];
 #pragma unroll
     for (int n = 0; n < NR; ++n)
@@ -798,7 +804,14 @@ __global__ __launch_bounds__(kThreads) void column_few(Args a, ColArgs p, int nb
 #pragma unroll
         for (int o = 1; o < 16; o <<= 1) v += __shfl_xor(v, o, 64);
         const int j = j0 + 16 * kb + 4 * g4 + r;
-        if (l16 == r && j < nkeys) to[j] = keep(j) ? v : 0.f;
+        if (l16 == r && j < nkeys) {
+          to[j] = keep(j) ? v : 0.f;
+          if (!PATH && !decltype(chunk)::value && p.acc.scores) {
+            const float sum = prior[kb] + v;
+            p.acc.scores[bh * a.M + j] = sum;
+            if (p.acc.copy) p.acc.copy[bh * a.M + j] = sum;
+          }
+        }
       }
   };
   auto consume = [&](int g, int u) H2O_INLINE {
@@ -820,7 +833,7 @@ __global__ __launch_bounds__(kThreads) void column_few(Args a, ColArgs p, int nb
       for (int r = 0; r < 4; ++r)
         ck[kb][r] = Q8 ? a.c * __shfl(ks[u], 16 * kb + 4 * g4 + r, 64) : a.c;
     }
-    columns(IntConst<0>{}, kf, ck, 32 * g, a.M, dst, [](int) { return true; });
+    columns(IntConst<0>{}, kf, ck, 32 * g, a.M, dst, old[u], [](int) { return true; });
   };
   // whole trips of two groups (one past the cache reads zeros and stores nothing): an
   // exit or a branch between the two makes the compiler wait for the loads in flight
@@ -849,20 +862,22 @@ __global__ __launch_bounds__(kThreads) void column_few(Args a, ColArgs p, int nb
         kf[kb][x] = *reinterpret_cast<const bf16x8*>(a.kn + row * D + 16 * g4 + 64 * (x >> 1) +
                                                      8 * (x & 1));
     }
-    columns(IntConst<1>{}, kf, ck, j0, p.A, dst + a.M,
+    columns(IntConst<1>{}, kf, ck, j0, p.A, dst + a.M, old[0],
             [&](int j) { return path_node(path, j, a.T) >= 0; });
   }
 }
 
 // wsum = the row ranges' sums, in their order.
 __global__ __launch_bounds__(kThreads) void column_reduce(const float* __restrict__ parts,
-                                                          float* __restrict__ wsum, size_t n,
-                                                          int nranges) {
-  const size_t e = (size_t)blockIdx.x * kThreads + threadIdx.x;
-  if (e >= n) return;
+                                                          float* __restrict__ wsum, int BH, int M,
+                                                          int A, int nranges, ScoreAcc acc) {
+  const int j = blockIdx.x * kThreads + threadIdx.x;
+  if (j >= M + A) return;
+  const size_t bh = blockIdx.y, e = bh * (size_t)(M + A) + j, n = (size_t)BH * (M + A);
   float s = parts[e];
   for (int k = 1; k < nranges; ++k) s += parts[k * n + e];
   wsum[e] = s;
+  if (j < M) acc.add(bh * M + j, s);
 }
 
 // ---------------------------------------------------------------------- tree
@@ -967,6 +982,8 @@ FlashPlan flash_plan(const FlashShape& s, bool tree) {
   const int nr = tree ? kMaxColumnRanges : p.nranges;
   const size_t parts = nr > 1 ? align256_size((size_t)nr * BH * (s.M + s.T) * sizeof(float)) : 0;
   if (p.off_parts + parts > off) off = p.off_parts + parts;
+  p.off_keys = off;
+  if (!tree) off = align256_size(off + (size_t)BH * s.M * sizeof(float));
   p.bytes = off;
   return p;
 }
@@ -1019,11 +1036,11 @@ hipError_t launch_flash_combine(const FlashShape& s, const FlashPlan& p, void* o
   return s.d == 64 ? go(IntConst<64>{}, bf16_t{}) : go(IntConst<128>{}, bf16_t{});
 }
 
-hipError_t launch_column_reduce(const float* parts, float* wsum, size_t n, int nranges,
-                                hipStream_t st) {
+hipError_t launch_column_reduce(const float* parts, float* wsum, int BH, int M, int A, int nranges,
+                                ScoreAcc acc, hipStream_t st) {
   return launch_kernel(K_COLUMN_REDUCE, column_reduce,
-                       dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), st, parts,
-                       wsum, n, nranges);
+                       dim3((unsigned)((M + A + kThreads - 1) / kThreads), BH), dim3(kThreads), st,
+                       parts, wsum, BH, M, A, nranges, acc);
 }
 
 hipError_t launch_flash(const FlashShape& s, const FlashPlan& p, const FlashIn& in, void* out,
@@ -1063,12 +1080,12 @@ hipError_t launch_flash(const FlashShape& s, const FlashPlan& p, const FlashIn& 
 
 hipError_t launch_columns(const FlashShape& s, const FlashPlan& p, const FlashIn& in,
                           const float* lse, const int32_t* path, int A, void* k_acc, void* v_acc,
-                          float* wsum, char* ws, float scale, hipStream_t st) {
+                          float* wsum, char* ws, float scale, hipStream_t st, ScoreAcc acc) {
   const Args a = make_args(s, in, ws, p, scale);
   float* parts = reinterpret_cast<float*>(ws + p.off_parts);
   const int ncol = path ? A : s.T;
   if (s.G() * ncol <= kFewRows) {
-    const ColArgs c{lse, path, ncol, s.G() * ncol, wsum, (bf16_t*)k_acc, (bf16_t*)v_acc};
+    const ColArgs c{lse, path, ncol, s.G() * ncol, wsum, (bf16_t*)k_acc, (bf16_t*)v_acc, acc};
     // blocks per head: as many as are resident (4 per CU, 3 with 64 rows), then as many
     // as give every wave one group of keys or an even count
     const int groups = (s.M + 31) / 32, most = (c.R <= 32 ? 4 : 3) * device_cus() / s.BH();
@@ -1094,7 +1111,7 @@ hipError_t launch_columns(const FlashShape& s, const FlashPlan& p, const FlashIn
   const int kb = 32 * nw, nt = 64 * nw, tiles = (s.M + kb - 1) / kb + (ncol + kb - 1) / kb;
   const int ncopy = path ? (A * (s.d / 8) + nt - 1) / nt : 0;
   const ColArgs c{lse, path, ncol, s.G() * ncol, p.nranges > 1 ? parts : wsum, (bf16_t*)k_acc,
-                  (bf16_t*)v_acc};
+                  (bf16_t*)v_acc, p.nranges > 1 ? ScoreAcc{} : acc};
   const dim3 grid(tiles + ncopy, s.BH(), p.nranges);
   const hipError_t e = with_cache(s.d, in.q8, [&](auto D, auto q) {
     constexpr int kD = decltype(D)::value;
@@ -1106,7 +1123,7 @@ hipError_t launch_columns(const FlashShape& s, const FlashPlan& p, const FlashIn
     return hipErrorInvalidValue;
   });
   if (e != hipSuccess || p.nranges == 1) return e;
-  return launch_column_reduce(parts, wsum, (size_t)s.BH() * (s.M + ncol), p.nranges, st);
+  return launch_column_reduce(parts, wsum, s.BH(), s.M, ncol, p.nranges, acc, st);
 }
 
 }  // namespace h2o

@@ -268,6 +268,7 @@ struct ColArgs {
   const int32_t* path;
   int A, R;
   float *dst, *k_acc, *v_acc;
+  ScoreAcc acc;
 };
 constexpr int kQRows = 32;
 
@@ -414,7 +415,10 @@ __global__ __launch_bounds__(kThreads) void column_f32(Args a, ColArgs p) {
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) v += __shfl_xor(v, o, 64);
     const int jj = j0 + 4 * g4 + r;
-    if (l16 == 0 && jj < nkeys) dst[jj] = PATH && !cache && node_of(jj) < 0 ? 0.f : v;
+    if (l16 == 0 && jj < nkeys) {
+      dst[jj] = PATH && !cache && node_of(jj) < 0 ? 0.f : v;
+      if (cache) p.acc.add(bh * a.M + jj, v);
+    }
   }
 }
 
@@ -460,14 +464,15 @@ hipError_t launch_flash_f32(const FlashShape& s, const FlashPlan& p, const Flash
 
 hipError_t launch_columns_f32(const FlashShape& s, const FlashPlan& p, const FlashIn& in,
                               const float* lse, const int32_t* path, int A, void* k_acc,
-                              void* v_acc, float* wsum, char* ws, float scale, hipStream_t st) {
+                              void* v_acc, float* wsum, char* ws, float scale, hipStream_t st,
+                              ScoreAcc acc) {
   const Args a = make_args(s, in, ws, p, scale);
   float* parts = reinterpret_cast<float*>(ws + p.off_parts);
   const int ncol = path ? A : s.T, kb = kColumnKeysF32;
   const int tiles = (s.M + kb - 1) / kb + (ncol + kb - 1) / kb;
   const int ncopy = path ? (A * (s.d / 4) + kThreads - 1) / kThreads : 0;
   const ColArgs c{lse, path, ncol, s.G() * ncol, p.nranges > 1 ? parts : wsum, (float*)k_acc,
-                  (float*)v_acc};
+                  (float*)v_acc, p.nranges > 1 ? ScoreAcc{} : acc};
   const dim3 grid(tiles + ncopy, s.BH(), p.nranges);
   const hipError_t e = with_cache(s.d, in.q8, [&](auto D, auto q) {
     constexpr int kD = decltype(D)::value;
@@ -480,7 +485,7 @@ hipError_t launch_columns_f32(const FlashShape& s, const FlashPlan& p, const Fla
     return hipErrorInvalidValue;
   });
   if (e != hipSuccess || p.nranges == 1) return e;
-  return launch_column_reduce(parts, wsum, (size_t)s.BH() * (s.M + ncol), p.nranges, st);
+  return launch_column_reduce(parts, wsum, s.BH(), s.M, ncol, p.nranges, acc, st);
 }
 
 }  // namespace h2o

@@ -80,6 +80,13 @@ struct KeyPos {
 struct ScoreAcc {
   float* scores = nullptr;
   float* copy = nullptr;
+  // adds slot `at` (of all heads)
+  __device__ __forceinline__ void add(size_t at, float w) const {
+    if (!scores) return;
+    const float s = scores[at] + w;
+    scores[at] = s;
+    if (copy) copy[at] = s;
+  }
 };
 
 // Packed row r of a KV head is (chunk position i = r / G, group member g = r % G).
@@ -311,6 +318,11 @@ hipError_t launch_kv_quantize(const void* k_src, const void* v_src, const int32_
                               hipStream_t st, float* scores = nullptr,
                               int32_t* token_pos = nullptr, const float* wsum = nullptr,
                               int T = 0, int32_t pos0 = 0);
+// launch_bottomk_insert into an 8-bit cache.
+hipError_t launch_bottomk_insert_q8(const float* keys, float* scores, int32_t* token_pos,
+                                    const CacheQ8& c, const void* kn, const void* vn,
+                                    const float* wsum, int32_t* idx, int rows, int M, int T, int d,
+                                    int k, int32_t pos0, bool f32, hipStream_t st);
 hipError_t launch_kv_dequantize(const CacheQ8& c, const int32_t* idx, void* k_dst, void* v_dst,
                                 int rows, int M, int k, int d, bool f32, hipStream_t st);
 
@@ -333,7 +345,9 @@ struct FlashPlan {
   int rows;                     // packed rows per block
   int nsplit;                   // key ranges
   int nranges;                  // row ranges of the column sums
-  size_t off_stats, off_opart, off_bits, off_parts, bytes;
+  size_t off_stats, off_opart, off_bits, off_parts;
+  size_t off_keys;              // [BH][M] floats, the ranking copy of a chunk step (not a tree's)
+  size_t bytes;
 };
 constexpr int kMaxFlashSplit = 32, kMaxColumnRanges = 8;
 constexpr int kColumnKeysF32 = 64;   // keys per block of the float32 column sums
@@ -350,14 +364,18 @@ hipError_t launch_tree_bits(const FlashShape& s, const FlashPlan& p, const int32
                             char* ws, hipStream_t st);
 // path null: wsum [BH][M + T] of all rows of the chunk, causal; else [BH][M + A] of
 // the path's A nodes, and their keys and values into k_acc and v_acc.
+// acc: the score accumulation of a chunk step in the same pass.
 hipError_t launch_columns(const FlashShape& s, const FlashPlan& p, const FlashIn& in,
                           const float* lse, const int32_t* path, int A, void* k_acc, void* v_acc,
-                          float* wsum, char* ws, float scale, hipStream_t st);
+                          float* wsum, char* ws, float scale, hipStream_t st,
+                          ScoreAcc acc = ScoreAcc{});
 hipError_t launch_columns_f32(const FlashShape& s, const FlashPlan& p, const FlashIn& in,
                               const float* lse, const int32_t* path, int A, void* k_acc,
-                              void* v_acc, float* wsum, char* ws, float scale, hipStream_t st);
-hipError_t launch_column_reduce(const float* parts, float* wsum, size_t n, int nranges,
-                                hipStream_t st);
+                              void* v_acc, float* wsum, char* ws, float scale, hipStream_t st,
+                              ScoreAcc acc = ScoreAcc{});
+// wsum [BH][M + A] from the row ranges' sums.
+hipError_t launch_column_reduce(const float* parts, float* wsum, int BH, int M, int A, int nranges,
+                                ScoreAcc acc, hipStream_t st);
 // T == 1 over an 8-bit cache, bf16 queries, a plan of path 2: the attention with
 // the summed weights, and the whole step with the h2o ranking.
 hipError_t launch_sdpa_decode_q8(const Shape& s, const Plan& p, const void* q, const CacheQ8& c,

@@ -122,5 +122,38 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t m) {
   return m;
 }
 
+// Values of a row that a lane has: 32 bytes.
+template <typename E>
+__host__ __device__ constexpr int per_lane() { return 32 / (int)sizeof(E); }
+
+// N / 4 words of codes.
+template <int N>
+__device__ __forceinline__ void store_codes(int8_t* p, const uint32_t (&c)[N / 4]) {
+  if constexpr (N == 16) *reinterpret_cast<u32x4*>(p) = u32x4{c[0], c[1], c[2], c[3]};
+  else *reinterpret_cast<uint2*>(p) = make_uint2(c[0], c[1]);
+}
+// A row of K and one of V into slot `dst` (of all heads) of an 8-bit cache, if ok; lane
+// `part` of the D / per_lane lanes that share the rows, which are all here.
+template <int D, typename E>
+__device__ __forceinline__ void put_rows(const CacheQ8& c, const E* k_src, const E* v_src,
+                                         size_t dst, bool ok, int part) {
+  constexpr int N = per_lane<E>(), LPR = D / N;
+  float x[N], y[N];
+  load_row<N>(x, k_src + N * part);
+  load_row<N>(y, v_src + N * part);
+  const float sx = row_scale(lanes_max<LPR>(amax_bits<N>(x)));
+  const float sy = row_scale(lanes_max<LPR>(amax_bits<N>(y)));
+  if (!ok) return;
+  uint32_t cx[N / 4], cy[N / 4];
+  quantize<N>(x, sx, cx);
+  quantize<N>(y, sy, cy);
+  store_codes<N>(c.k + dst * D + N * part, cx);
+  store_codes<N>(c.v + dst * D + N * part, cy);
+  if (part == 0) {
+    c.ks[dst] = sx;
+    c.vs[dst] = sy;
+  }
+}
+
 }  // namespace q8
 }  // namespace h2o

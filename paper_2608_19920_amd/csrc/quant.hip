@@ -28,15 +28,6 @@ struct InsertArgs {
   int32_t pos0;
 };
 
-template <typename E>
-__host__ __device__ constexpr int per_lane() { return 32 / (int)sizeof(E); }
-
-// N / 4 words of codes.
-template <int N>
-__device__ __forceinline__ void store_codes(int8_t* p, const uint32_t (&c)[N / 4]) {
-  if constexpr (N == 16) *reinterpret_cast<u32x4*>(p) = u32x4{c[0], c[1], c[2], c[3]};
-  else *reinterpret_cast<uint2*>(p) = make_uint2(c[0], c[1]);
-}
 template <int N>
 __device__ __forceinline__ void load_codes(uint32_t (&c)[N / 4], const int8_t* p) {
   if constexpr (N == 16) {
@@ -55,32 +46,19 @@ __global__ __launch_bounds__(kThreads) void quantize_rows(
     const E* __restrict__ k_src, const E* __restrict__ v_src, const int32_t* __restrict__ idx,
     int8_t* __restrict__ kc, float* __restrict__ ks, int8_t* __restrict__ vc,
     float* __restrict__ vs, uint32_t nrows, int M, uint32_t k, InsertArgs ins) {
-  constexpr int N = per_lane<E>(), LPR = D / N;
+  constexpr int LPR = D / per_lane<E>();
   const uint32_t row = blockIdx.x * (kThreads / LPR) + threadIdx.x / LPR;
   if (row >= nrows) return;   // whole rows: the lanes of a row leave together
   const int part = threadIdx.x % LPR;
   const uint32_t bh = row / k, i = row % k;
-  const size_t src = (size_t)row * D + N * part;
-  float x[N], y[N];
-  load_row<N>(x, k_src + src);
-  load_row<N>(y, v_src + src);
   const int slot = idx ? idx[row] : (int)i;
-  const float sx = row_scale(lanes_max<LPR>(amax_bits<N>(x)));
-  const float sy = row_scale(lanes_max<LPR>(amax_bits<N>(y)));
-  if ((unsigned)slot >= (unsigned)M) return;
-  uint32_t cx[N / 4], cy[N / 4];
-  quantize<N>(x, sx, cx);
-  quantize<N>(y, sy, cy);
+  const bool ok = (unsigned)slot < (unsigned)M;
   const size_t dst = (size_t)bh * M + slot;
-  store_codes<N>(kc + dst * D + N * part, cx);
-  store_codes<N>(vc + dst * D + N * part, cy);
-  if (part == 0) {
-    ks[dst] = sx;
-    vs[dst] = sy;
-    if (ins.scores) {
-      ins.scores[dst] = ins.wsum[(size_t)bh * (M + ins.T) + M + i];
-      if (ins.token_pos) ins.token_pos[dst] = ins.pos0 + (int32_t)i;
-    }
+  put_rows<D, E>(CacheQ8{kc, ks, vc, vs}, k_src + (size_t)row * D, v_src + (size_t)row * D, dst, ok,
+                 part);
+  if (ok && part == 0 && ins.scores) {
+    ins.scores[dst] = ins.wsum[(size_t)bh * (M + ins.T) + M + i];
+    if (ins.token_pos) ins.token_pos[dst] = ins.pos0 + (int32_t)i;
   }
 }
 

@@ -1,6 +1,7 @@
 // Column-sum reduce, H2O score accumulation, bottom-k selection and insert.
 #include "colsum.h"
 #include "internal.h"
+#include "q8.h"
 
 namespace h2o {
 namespace {
@@ -394,12 +395,12 @@ __global__ __launch_bounds__(kSelThreads) void bottomk_kernel(const float* __res
 // as bottomk_kernel followed by insert_kernel.
 // keys_in may be the scores themselves with X = 1 and LDS: the block has its
 // row in LDS before it writes a score.
-template <bool LDS>
-__global__ __launch_bounds__(kSelThreads) void bottomk_insert_kernel(
-    const float* keys_in, float* scores,
-    int32_t* __restrict__ token_pos, uint4* __restrict__ kc, uint4* __restrict__ vc,
-    const uint4* __restrict__ kn, const uint4* __restrict__ vn, const float* __restrict__ wsum,
-    int32_t* __restrict__ idx, int M, int T, int k, int vecs, int32_t pos0) {
+// copy(row, sidx, i0, i1) copies chunk tokens [i0, i1) of the row into slots sidx[i].
+template <bool LDS, typename Copy>
+__device__ __forceinline__ void bottomk_insert_body(
+    const float* keys_in, float* scores, int32_t* __restrict__ token_pos,
+    const float* __restrict__ wsum, int32_t* __restrict__ idx, int M, int T, int k, int32_t pos0,
+    Copy&& copy) {
   __shared__ uint32_t keys[LDS ? kSelLdsMax + kSelLdsMax / 32 : 1];
   __shared__ uint32_t hist[kSelBins];
   __shared__ uint32_t tmp[2 * kSelWaves + 1];
@@ -422,36 +423,63 @@ __global__ __launch_bounds__(kSelThreads) void bottomk_insert_kernel(
     }
   });
   __syncthreads();
-  // chunk tokens [i0, i1) of this block: 16-byte vectors, four loads of each
-  // tensor in flight per thread before the stores
-  const int i0 = (int)((long long)k * x / X), i1 = (int)((long long)k * (x + 1) / X);
-  const int n = (i1 - i0) * vecs;
-  constexpr int U = 4;
-  for (int e0 = threadIdx.x; e0 < n; e0 += U * kSelThreads) {
-    uint4 kv[U], vv[U];
-    uint32_t slot[U];
-    int cc[U];
+  copy(row, sidx, (int)((long long)k * x / X), (int)((long long)k * (x + 1) / X));
+}
+
+template <bool LDS>
+__global__ __launch_bounds__(kSelThreads) void bottomk_insert_kernel(
+    const float* keys_in, float* scores,
+    int32_t* __restrict__ token_pos, uint4* __restrict__ kc, uint4* __restrict__ vc,
+    const uint4* __restrict__ kn, const uint4* __restrict__ vn, const float* __restrict__ wsum,
+    int32_t* __restrict__ idx, int M, int T, int k, int vecs, int32_t pos0) {
+  bottomk_insert_body<LDS>(
+      keys_in, scores, token_pos, wsum, idx, M, T, k, pos0,
+      [&](size_t row, const uint32_t* sidx, int i0, int i1) {
+        // 16-byte vectors, four loads of each tensor in flight per thread before the stores
+        const int n = (i1 - i0) * vecs;
+        constexpr int U = 4;
+        for (int e0 = threadIdx.x; e0 < n; e0 += U * kSelThreads) {
+          uint4 kv[U], vv[U];
+          uint32_t slot[U];
+          int cc[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int e = e0 + u * kSelThreads;
-      slot[u] = 0xFFFFFFFFu;
-      cc[u] = 0;
-      if (e < n) {
-        const int i = i0 + e / vecs;
-        cc[u] = e % vecs;
-        kv[u] = kn[(row * T + i) * vecs + cc[u]];
-        vv[u] = vn[(row * T + i) * vecs + cc[u]];
-        slot[u] = sidx[i];
-      }
-    }
+          for (int u = 0; u < U; ++u) {
+            const int e = e0 + u * kSelThreads;
+            slot[u] = 0xFFFFFFFFu;
+            cc[u] = 0;
+            if (e < n) {
+              const int i = i0 + e / vecs;
+              cc[u] = e % vecs;
+              kv[u] = kn[(row * T + i) * vecs + cc[u]];
+              vv[u] = vn[(row * T + i) * vecs + cc[u]];
+              slot[u] = sidx[i];
+            }
+          }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (slot[u] < (uint32_t)M) {
-        kc[(row * M + slot[u]) * vecs + cc[u]] = kv[u];
-        vc[(row * M + slot[u]) * vecs + cc[u]] = vv[u];
-      }
-    }
-  }
+          for (int u = 0; u < U; ++u) {
+            if (slot[u] < (uint32_t)M) {
+              kc[(row * M + slot[u]) * vecs + cc[u]] = kv[u];
+              vc[(row * M + slot[u]) * vecs + cc[u]] = vv[u];
+            }
+          }
+        }
+      });
+}
+
+// The same into an 8-bit cache: the rows of quantize_rows, a row per D / N lanes.
+template <bool LDS, int D, typename E>
+__global__ __launch_bounds__(kSelThreads) void bottomk_insert_q8(
+    const float* keys_in, float* scores, int32_t* __restrict__ token_pos, CacheQ8 c8,
+    const E* __restrict__ kn, const E* __restrict__ vn, const float* __restrict__ wsum,
+    int32_t* __restrict__ idx, int M, int T, int k, int32_t pos0) {
+  bottomk_insert_body<LDS>(
+      keys_in, scores, token_pos, wsum, idx, M, T, k, pos0,
+      [&](size_t row, const uint32_t* sidx, int i0, int i1) {
+        constexpr int LPR = D / q8::per_lane<E>();
+        for (int i = i0 + (int)threadIdx.x / LPR; i < i1; i += kSelThreads / LPR)
+          q8::put_rows<D, E>(c8, kn + (row * T + i) * (size_t)D, vn + (row * T + i) * (size_t)D,
+                             row * M + sidx[i], sidx[i] < (uint32_t)M, threadIdx.x % LPR);
+      });
 }
 
 // -------------------------------------------------------------------- insert
@@ -705,6 +733,32 @@ hipError_t launch_bottomk_insert(const float* keys, float* scores, int32_t* toke
   return launch_kernel(K_BOTTOMK_INSERT, bottomk_insert_kernel<false>, grid, dim3(kSelThreads), st,
                        keys, scores, token_pos, (uint4*)kc, (uint4*)vc, (const uint4*)kn,
                        (const uint4*)vn, wsum, idx, M, T, k, vecs, pos0);
+}
+
+hipError_t launch_bottomk_insert_q8(const float* keys, float* scores, int32_t* token_pos,
+                                    const CacheQ8& c, const void* kn, const void* vn,
+                                    const float* wsum, int32_t* idx, int rows, int M, int T, int d,
+                                    int k, int32_t pos0, bool f32, hipStream_t st) {
+  if (rows == 0 || k == 0) return hipSuccess;
+  if (!bottomk_insert_supported(k)) return hipErrorInvalidValue;
+  int X = 256 / rows;   // as launch_bottomk_insert
+  if (X > 32) X = 32;
+  if (X < 1) X = 1;
+  if (keys == scores) {
+    if (!bottomk_insert_in_place(M, k, d, f32 ? 4 : 2)) return hipErrorInvalidValue;
+    X = 1;
+  }
+  auto go = [&](auto D, auto e) {
+    typedef decltype(e) E;
+    constexpr int kD = decltype(D)::value;
+    return launch_kernel(K_BOTTOMK_INSERT,
+                         M <= kSelLdsMax ? bottomk_insert_q8<true, kD, E>
+                                         : bottomk_insert_q8<false, kD, E>,
+                         dim3(rows, X), dim3(kSelThreads), st, keys, scores, token_pos, c,
+                         (const E*)kn, (const E*)vn, wsum, idx, M, T, k, pos0);
+  };
+  if (d == 64) return f32 ? go(IntConst<64>{}, float{}) : go(IntConst<64>{}, bf16_t{});
+  return f32 ? go(IntConst<128>{}, float{}) : go(IntConst<128>{}, bf16_t{});
 }
 
 hipError_t launch_insert(void* kc, void* vc, float* scores, int32_t* token_pos, const void* kn,
