@@ -343,7 +343,8 @@ int h2o_kv_scatter(void* cache, const int32_t* idx, const void* src, int B,
  *   code * scale, off x by at most scale / 2 (plus the scale's own rounding).
  * A row whose scale would be below 2^-126 (the smallest normal float32) is held as
  * zeros with scale 0. A row with an Inf or NaN has scale NaN and codes 0: it reads
- * back as NaN, and a query that attends it gets NaN.
+ * back as NaN, and a query that attends it gets NaN. (A row that holds the largest
+ * finite float32 reads back as Inf there: its scale is rounded up.)
  * dtype is that of the rows on the other side (q, k_new, v_new, out, ...). All
  * limits of the shapes above hold; B * Hkv <= 65535 where there are queries, and
  * B * Hkv * k < 2^28 rows. */
@@ -407,7 +408,9 @@ int h2o_chunk_step_q8(const void* q, int8_t* k_codes, float* k_scales,
  * tokens are nodes: parents [B,T] int32 holds for node i its parent's index, in
  * [0, i), or -1 where it follows the last token before the draft (other values
  * count as -1). A node sees every cache slot, its ancestors and itself; a chain
- * (parents i - 1) is the causal chunk.
+ * (parents i - 1) is the causal chunk. Where a batch entry has fewer than T nodes,
+ * the others are filled with nodes of finite values that none has as its parent (in
+ * float32 of any values, see above); their out and lse mean nothing.
  *
  * The cache is in dtype (k_scales and v_scales NULL) or in 8 bits (k_cache and
  * v_cache are int8 codes, both scales given). */

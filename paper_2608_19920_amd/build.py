@@ -33,9 +33,9 @@ FLAGS = [
 # are -inf), so max() needs no NaN quieting.
 FILE_FLAGS = {
     "decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-    "sdpa_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"],
+    "sdpa_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "f32_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-    "flash.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"],
+    "flash.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "flash_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "backward_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }

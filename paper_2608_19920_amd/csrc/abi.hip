@@ -1002,8 +1002,8 @@ int check_attend_q8(const void* q, const CacheQ8& c, const void* k_new, const vo
 }
 
 // The attention with the summed weights. scores non-null: these are added to them, by
-// the column sums where they are a kernel of their own; keys non-null as well: set to a
-// copy of the accumulated scores, or to the scores where there is none.
+// the column sums where they are a kernel of their own; keys non-null as well (not with
+// the token kernels): set to a copy of the accumulated scores.
 hipError_t launch_attend_q8(const void* q, const CacheQ8& c, const void* k_new, const void* v_new,
                             void* out, float* lse, float* wsum, char* ws, int B, int Hq, int Hkv,
                             int T, int M, int d, float scale, int dtype, hipStream_t st,
@@ -1013,7 +1013,6 @@ hipError_t launch_attend_q8(const void* q, const CacheQ8& c, const void* k_new, 
     hipError_t e = launch_sdpa_decode_q8(s, path_plan(s, 2), q, c, k_new, v_new, out, lse, wsum, ws,
                                          scale, st);
     if (e == hipSuccess && scores) e = launch_accumulate(scores, wsum, B * Hkv, M, T, st);
-    if (keys) *keys = scores;
     return e;
   }
   const FlashShape s{B, Hq, Hkv, T, M, d, dtype == H2O_F32};
@@ -1158,8 +1157,8 @@ int h2o_evict_insert_q8(int8_t* k_codes, float* k_scales, int8_t* v_codes, float
   if (!aligned16(workspace)) return fail(H2O_EALIGN, "workspace not 16-byte aligned");
   rc = check_device();
   if (rc) return rc;
-  return launched(launch_evict_q8(policy, c, scores, scores, token_pos, k_new, v_new, wsum, evict_idx, B,
-                                  Hkv, M, T, d, k, pos0, pos0 + T, dtype == H2O_F32,
+  return launched(launch_evict_q8(policy, c, scores, scores, token_pos, k_new, v_new, wsum,
+                                  evict_idx, B, Hkv, M, T, d, k, pos0, pos0 + T, dtype == H2O_F32,
                                   reinterpret_cast<char*>(workspace),
                                   reinterpret_cast<hipStream_t>(stream)));
 }

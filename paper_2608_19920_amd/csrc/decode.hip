@@ -1312,8 +1312,8 @@ hipError_t launch_finish(const Shape& s, const Plan& p, bool out_too, int ns, co
                                         scores, nullptr, true, ws, c, st);
     if (e != hipSuccess) return e;
     return launch_kernel(K_DECODE_INSERT, c8 ? decode_insert<true> : decode_insert<false>,
-                         dim3(s.BH()), dim3(64), st, (bf16_t*)kc, (bf16_t*)vc, to, (const bf16_t*)kn, (const bf16_t*)vn, s.d, s.M,
-                         (s.M + kCombSlots - 1) / kCombSlots, (const uint2*)(ws + p.off_keys),
+                         dim3(s.BH()), dim3(64), st, (bf16_t*)kc, (bf16_t*)vc, to,
+                         (const bf16_t*)kn, (const bf16_t*)vn, s.d, s.M, (s.M + kCombSlots - 1) / kCombSlots, (const uint2*)(ws + p.off_keys),
                          (const float*)wsum, scores, token_pos, evict_idx, pos0);
   }
   auto go = [&](auto kern) {
@@ -1385,8 +1385,8 @@ hipError_t launch_decode_split_q8(const Shape& s, const Plan& p, const void* q, 
     constexpr int D = decltype(d)::value, G = decltype(g)::value;
     *ns = split_count<D, G, false, false, true>(s.M, s.BH());
     const bool nt = (size_t)s.BH() * s.M * (size_t)(2 * D) >= kNtBytes;
-    return launch_kernel(K_DECODE_SPLIT, nt ? decode_split_q8<D, G, true> : decode_split_q8<D, G, false>,
-                         dim3(*ns, s.BH()), dim3(kThreads), st, (const bf16_t*)q,
+    return launch_kernel(K_DECODE_SPLIT,
+                         nt ? decode_split_q8<D, G, true> : decode_split_q8<D, G, false>, dim3(*ns, s.BH()), dim3(kThreads), st, (const bf16_t*)q,
                          (const int8_t*)c8.k, (const float*)c8.ks, (const int8_t*)c8.v,
                          (const float*)c8.vs, s.Hq, s.Hkv, s.M, c,
                          reinterpret_cast<float*>(ws + p.off_logits),

@@ -112,7 +112,8 @@ __device__ __forceinline__ void store_rows8(bf16_t* lds, const u32x4* r) {
   for (int e = 0; e < Regs<D, NT, BN>::N8; ++e) {
     const int u = threadIdx.x + e * NT;
     if (BN * D / 16 < NT && u >= BN * D / 16) return;
-    bf16x8* dst = reinterpret_cast<bf16x8*>(lds + u / (D / 16) * lds_pitch(D) + 16 * (u % (D / 16)));
+    bf16x8* dst =
+        reinterpret_cast<bf16x8*>(lds + u / (D / 16) * lds_pitch(D) + 16 * (u % (D / 16)));
     dst[0] = q8::codes_bf16(r[e][0], r[e][1]);
     dst[1] = q8::codes_bf16(r[e][2], r[e][3]);
   }
@@ -121,7 +122,8 @@ __device__ __forceinline__ void store_rows8(bf16_t* lds, const u32x4* r) {
 // Rows past the tile's end re-read its last row (in bounds; masked later).
 // WHOLE: the caller knows that it is a whole cache tile (no branch).
 template <int D, bool Q8, int NT, int BN, bool WHOLE = false>
-__device__ __forceinline__ void load_tile(Regs<D, NT, BN>& g, const Args& a, size_t bh, int t, int tc) {
+__device__ __forceinline__ void load_tile(Regs<D, NT, BN>& g, const Args& a, size_t bh, int t,
+                                          int tc) {
   if (WHOLE || t < tc) {
     const int j0 = t * BN, n = WHOLE ? BN : min(BN, a.M - j0);
     const size_t row = bh * (size_t)a.M + j0;
@@ -287,7 +289,8 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
           if (MASK) {
             const int j = 16 * kb + 4 * g4 + r;
             const bool hid = cache ? t * BN + j >= a.M
-                             : TREE ? !((seen[n][kb >> 1] >> (j & 31)) & 1u) : (t - tc) * BN + j > qi[n];
+                             : TREE ? !((seen[n][kb >> 1] >> (j & 31)) & 1u)
+                                    : (t - tc) * BN + j > qi[n];
             if (hid) v = -INFINITY;
           }
           x[4 * kb + r] = v;
@@ -599,7 +602,8 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void column_pass(Args a, 
       qr[e] = *reinterpret_cast<const u32x4*>(qh + (uint32_t)(rg[e] * a.T + n) * (uint32_t)D);
       advance(ri[e], rg[e]);
     }
-    if (tid < kQRows) {   // a row that is none: lambda +inf, weights 0
+    if (tid < kQRows) {   // a row that is none: lambda +inf, weights 0 (of a path: not added
+                          // at all, whatever query was read in its place)
       const int n = li < p.A ? node_of(li) : -1;
       lr = n >= 0 ? lh[lg * a.T + n] * kLog2e : INFINITY;
       ir = li;
@@ -643,6 +647,7 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void column_pass(Args a, 
     for (int n = 0; n < kQRows / 16; ++n) {
       if (n + 1 < kQRows / 16) product(s[(n + 1) & 1], n + 1);
       const float la = lam[buf][16 * n + l16];
+      if (PATH && la == INFINITY) continue;
       const int i = decltype(chunk)::value ? pos[buf][16 * n + l16] : 0;
 #pragma unroll
       for (int kb = 0; kb < NKB; ++kb)
@@ -786,6 +791,7 @@ __global__ __launch_bounds__(kThreads) void column_few(Args a, ColArgs p, int nb
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
       const float la = lam[16 * n + l16];
+      if (PATH && la == INFINITY) continue;
       const int i = decltype(chunk)::value ? (16 * n + l16) / a.G : 0;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -925,8 +931,8 @@ hipError_t with_cache(int d, bool q8, F&& f) {
 Args make_args(const FlashShape& s, const FlashIn& in, const char* ws, const FlashPlan& p,
                float scale) {
   return Args{(const bf16_t*)in.q, in.kc, in.vc, in.ks, in.vs, (const bf16_t*)in.kn,
-              (const bf16_t*)in.vn, in.parents, reinterpret_cast<const uint32_t*>(ws + p.off_bits), s.Hq, s.Hkv,
-              s.G(), s.T, s.M, s.G() * s.T, (s.T + 31) / 32, scale * kLog2e};
+              (const bf16_t*)in.vn, in.parents, reinterpret_cast<const uint32_t*>(ws + p.off_bits),
+              s.Hq, s.Hkv, s.G(), s.T, s.M, s.G() * s.T, (s.T + 31) / 32, scale * kLog2e};
 }
 
 }  // namespace
@@ -1013,9 +1019,8 @@ hipError_t launch_tree_bits(const FlashShape& s, const FlashPlan& p, const int32
   uint32_t* bits = reinterpret_cast<uint32_t*>(ws + p.off_bits);
   const int W = (s.T + 31) / 32;
   const dim3 grid((s.T + kThreads - 1) / kThreads, s.B);
-  return s.T <= kTreeLds
-             ? launch_kernel(K_TREE_BITS, tree_bits<true>, grid, dim3(kThreads), st, parents, s.T, W, bits)
-             : launch_kernel(K_TREE_BITS, tree_bits<false>, grid, dim3(kThreads), st, parents, s.T, W, bits);
+  return launch_kernel(K_TREE_BITS, s.T <= kTreeLds ? tree_bits<true> : tree_bits<false>, grid,
+                       dim3(kThreads), st, parents, s.T, W, bits);
 }
 
 hipError_t launch_flash_combine(const FlashShape& s, const FlashPlan& p, void* out, float* lse,
@@ -1060,8 +1065,7 @@ hipError_t launch_flash(const FlashShape& s, const FlashPlan& p, const FlashIn& 
     constexpr bool kQ = decltype(q)::value;
     auto go = [&](auto kern) {
       return launch_kernel(K_FLASH, kern, grid, dim3(p.rows == 256 ? 512 : 256), st, a, p.nsplit,
-                           (bf16_t*)out, lse,
-                           stats, opart);
+                           (bf16_t*)out, lse, stats, opart);
     };
     auto rows = [&](auto mask) {
       constexpr bool kT = decltype(mask)::value;
@@ -1117,9 +1121,11 @@ hipError_t launch_columns(const FlashShape& s, const FlashPlan& p, const FlashIn
     constexpr int kD = decltype(D)::value;
     constexpr bool kQ = decltype(q)::value;
     auto go = [&](auto kern) { return launch_kernel(K_COLUMNS, kern, grid, dim3(nt), st, a, c); };
-    if (path) return nw == 8 ? go(column_pass<kD, kQ, true, 2, 8>) : go(column_pass<kD, kQ, true, 2, 4>);
+    if (path)
+      return nw == 8 ? go(column_pass<kD, kQ, true, 2, 8>) : go(column_pass<kD, kQ, true, 2, 4>);
     if constexpr (kQ)
-      return nw == 8 ? go(column_pass<kD, true, false, 2, 8>) : go(column_pass<kD, true, false, 2, 4>);
+      return nw == 8 ? go(column_pass<kD, true, false, 2, 8>)
+                     : go(column_pass<kD, true, false, 2, 4>);
     return hipErrorInvalidValue;
   });
   if (e != hipSuccess || p.nranges == 1) return e;

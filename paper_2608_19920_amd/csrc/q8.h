@@ -50,7 +50,8 @@ __device__ __forceinline__ float row_scale(uint32_t amax_bits) {
 // it reaches half a scale the code is settled by it. That is rare, so it is
 // tested for all N at once.
 template <int N>
-__device__ __forceinline__ void quantize(const float (&x)[N], float scale, uint32_t (&codes)[N / 4]) {
+__device__ __forceinline__ void quantize(const float (&x)[N], float scale,
+                                         uint32_t (&codes)[N / 4]) {
   constexpr float kMagic = 12582912.f;   // 1.5 * 2^23
   if (!(scale > 0.f)) {   // zeros, or a row with an Inf or NaN
 #pragma unroll

@@ -5,7 +5,8 @@
 // bytes are written, or the reverse. A lane has kPer consecutive values of K and the
 // same of V, 32 bytes each: loads and stores of both tensors in flight together, the
 // row's maximum by exchanges between its lanes, no LDS and no barrier. (Float32 with 16
-// values a lane, 64 bytes: B3 Hkv16 d64, 3,001 rows written and read back 49 us, with 8 42.) B4 Hkv8 d128 bf16, 32,768 rows: 300 us for both calls, 5.4 TB/s.
+// values a lane, 64 bytes: B3 Hkv16 d64, 3,001 rows written and read back 49 us, with 8
+// 42.) B4 Hkv8 d128 bf16, 32,768 rows: 300 us for both calls, 5.4 TB/s.
 #include "internal.h"
 #include "q8.h"
 

@@ -7,6 +7,7 @@ import torch
 import oracle
 from paper_2608_19920_amd import h2o as H
 import _gpu as U
+import test_gpu_q8 as steps
 from _q8tree import close, dev, dev_cache, inputs
 
 pytestmark = pytest.mark.gpu
@@ -154,3 +155,15 @@ def test_two_streams_at_once():
     for g, w in zip(got, want):
         for a, b in zip(g, w):
             assert torch.equal(a, b)
+
+
+@pytest.mark.slow
+@pytest.mark.parametrize("case", [
+    (1, 2, 1, 64, 4500, 4100, "bf16", "h2o", True),      # more rows than one launch selects
+    (1, 2, 2, 64, 4300, 4200, "f32", "h2o_norm", True),
+    (2, 4, 2, 64, 40000, 3, "bf16", "h2o", True),        # a head's scores beyond LDS
+    (1, 8, 2, 128, 33000, 300, "bf16", "h2o_norm", True),
+    (2, 6, 3, 128, 9000, 1, "bf16", "h2o_orig", True),
+], ids=lambda c: "-".join(map(str, c)))
+def test_steps_of_many_rows_and_slots(case):
+    steps.test_step_is_its_three_parts(case)

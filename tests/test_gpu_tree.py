@@ -214,3 +214,35 @@ def test_captured_drafts_between_eager_ones():
         torch.cuda.synchronize()
         for k in ("out", "lse", "ka", "va", "wsum"):
             assert torch.equal(one[k], two[k]), (n, k)
+
+
+@pytest.mark.parametrize("dtype,q8", [("bf16", False), ("bf16", True), ("f32", False), ("f32", True)])
+@pytest.mark.parametrize("G,A", [(4, 3), (4, 14), (4, 30)])
+def test_a_batch_entry_without_tokens_gets_zeros(G, A, dtype, q8):
+    """A path that holds no token: weights, keys and values 0, whatever stands in the
+    entry's queries, keys, lse and cache; the other entries are as without it."""
+    B, Hkv, d, M, T = 3, 2, 64, 150, 40
+    x, tdt = inputs(B, Hkv * G, Hkv, d, M, T, dtype, seed=A), U.TDT[dtype]
+    parents = _parents("chain", B, T, None)
+    o, l = oracle.sdpa_tree(x["q"], x["k_values" if q8 else "k_cache"],
+                            x["v_values" if q8 else "v_cache"], x["k_new"], x["v_new"], parents,
+                            x["scale"])
+    path = np.tile(np.arange(A), (B, 1)).astype(np.int32)
+    path[1] = -1
+    w, k, v = oracle.tree_accept(x["q"], x["k_values" if q8 else "k_cache"], x["k_new"], x["v_new"],
+                                 l, path, x["scale"])
+    for n in ("q", "k_new", "v_new", "k_cache", "k_scales"):
+        x[n][1] = np.nan
+    l[1] = np.nan
+    c = dev_cache(x) if q8 else [dev(x["k_cache"], tdt), None]
+    ka, va = (torch.empty(B, Hkv, A, d, dtype=tdt, device=U.DEV) for _ in range(2))
+    wsum = torch.empty(B, Hkv, M + A, device=U.DEV)
+    ws = torch.full((max(16, H.h2o_tree_workspace_bytes(B, Hkv * G, Hkv, T, M, d, tdt)),), 255,
+                    dtype=torch.uint8, device=U.DEV)
+    H.h2o_tree_accept(dev(x["q"], tdt), c[0], dev(x["k_new"], tdt), dev(x["v_new"], tdt),
+                      dev(l.astype(np.float32)), dev(path), ka, va, wsum, ws, float(x["scale"]),
+                      k_scales=c[1])
+    assert not wsum[1].any() and not ka[1].any() and not va[1].any()
+    np.testing.assert_array_equal(U.to_np(ka), k)
+    np.testing.assert_array_equal(U.to_np(va), v)
+    close(dtype, "empty path", wsum=(wsum, w))
