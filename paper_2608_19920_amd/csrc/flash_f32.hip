@@ -19,6 +19,7 @@ using q8::u32x4;
 constexpr int BN = 32;          // keys per tile
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
+constexpr int kVmem0 = 0x0F70;  // s_waitcnt vmcnt(0)
 
 __device__ __forceinline__ f32x4 mma4(float a, float b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
@@ -155,7 +156,12 @@ __global__ __launch_bounds__(kThreads) void flash_f32(Args a, int nsplit, float*
   };
   if (threadIdx.x < 3) odd[threadIdx.x] = 0;
   __syncthreads();
+  auto word = [&](int t) {   // the chunk keys of tile t that the row's node sees
+    return t >= tc ? a.bits[((size_t)b * a.T + i) * a.W + (t - tc)] : 0u;
+  };
+  uint32_t next = 0u;
   if (t0 < t1) {
+    if constexpr (TREE) next = word(t0);
     load_tile<D, Q8>(g, a, bh, t0, tc);
     put(t0);
     if (t0 + 1 < t1) load_tile<D, Q8>(g, a, bh, t0 + 1, tc);
@@ -163,15 +169,20 @@ __global__ __launch_bounds__(kThreads) void flash_f32(Args a, int nsplit, float*
   for (int t = t0; t < t1; ++t) {
     const bool cache = t < tc;
     __syncthreads();                // tile t is in LDS, tile t - 1 used up
+    // tile t + 1 and the tree's word of tile t are here: a wait for the word where it is
+    // used would be one for tile t + 2 as well (B1 Hq32 Hkv8 d128 M8192, 32 nodes: 62 ->
+    // 59 us; a chunk, which has no such word, is slower with it, 203 -> 212)
+    if constexpr (TREE) __builtin_amdgcn_s_waitcnt(kVmem0);
     if (threadIdx.x == 0) odd[(t - t0 + 2) % 3] = 0;
     const float* Ks = Ks2[(t - t0) & 1];
     const float* Vs = Vs2[(t - t0) & 1];
     const bool finite = !odd[(t - t0) % 3];
+    const uint32_t seen = next;
     if (t + 1 < t1) {
       put(t + 1);
+      if constexpr (TREE) next = word(t + 1);
       if (t + 2 < t1) load_tile<D, Q8>(g, a, bh, t + 2, tc);
     }
-    const uint32_t seen = TREE && !cache ? a.bits[((size_t)b * a.T + i) * a.W + (t - tc)] : 0u;
     f32x4 s[NK];
     uint32_t hidden = 0u;
     float mn = m;
