@@ -30,7 +30,6 @@ using namespace mfma;
 
 constexpr int kThreads = 256;
 constexpr int kXcds = 8;
-constexpr int kWaveTree = 64;   // nodes of a tree that a wave masks by itself
 constexpr int kFewSplits = 4;   // key ranges that one thread merges alone
 // A lambda over register arrays: a call that is not inlined would put them in memory.
 #define H2O_INLINE __attribute__((always_inline))
@@ -225,20 +224,9 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
     for (int db = 0; db < D / 16; ++db) oacc[db][n] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // A tree of at most 64 nodes: lane i follows node i up by doubling its way, and a
-  // row's lanes take the node's bits.
-  uint64_t own[NQB];
+  uint64_t own[NQB];   // the ancestors of a tree of at most 64 nodes
   if (TREE && a.T <= kWaveTree) {
-    int up = lane < a.T ? a.parents[(size_t)b * a.T + lane] : -1;
-    if (up < 0 || up >= lane) up = -1;
-    uint64_t mine = 1ull << lane;
-#pragma unroll 1
-    for (int reach = 1; reach < a.T; reach *= 2) {
-      const uint64_t more = __shfl(mine, up < 0 ? lane : up, 64);
-      const int next = __shfl(up, up < 0 ? lane : up, 64);
-      mine |= more;
-      up = up < 0 ? -1 : next;
-    }
+    const uint64_t mine = wave_ancestors(a.parents + (size_t)b * a.T, a.T, lane);
 #pragma unroll
     for (int n = 0; n < NQB; ++n) own[n] = __shfl(mine, qi[n], 64);
   }
@@ -981,7 +969,7 @@ FlashPlan flash_plan(const FlashShape& s, bool tree) {
   p.off_opart = off;
   if (p.nsplit > 1) off = align256_size(off + (size_t)p.nsplit * BH * R * s.d * sizeof(float));
   p.off_bits = off;
-  if (tree && (s.f32 || s.T > kWaveTree))
+  if (tree && s.T > kWaveTree)
     off = align256_size(off + (size_t)s.B * s.T * ((s.T + 31) / 32) * 4);
   // the tree's column sums are a call of their own, of any path
   p.off_parts = tree ? 0 : off;

@@ -34,6 +34,7 @@ struct Args {
   const void *kc, *vc;
   const float *ks, *vs;
   const float *kn, *vn;
+  const int32_t* parents;
   const uint32_t* bits;
   int Hq, Hkv, G, T, M, R, W;
   float c;
@@ -156,8 +157,14 @@ __global__ __launch_bounds__(kThreads) void flash_f32(Args a, int nsplit, float*
   };
   if (threadIdx.x < 3) odd[threadIdx.x] = 0;
   __syncthreads();
+  uint64_t own = 0u;
+  if constexpr (TREE)
+    if (a.T <= kWaveTree)
+      own = __shfl(wave_ancestors(a.parents + (size_t)b * a.T, a.T, lane), i, 64);
   auto word = [&](int t) {   // the chunk keys of tile t that the row's node sees
-    return t >= tc ? a.bits[((size_t)b * a.T + i) * a.W + (t - tc)] : 0u;
+    if (t < tc) return 0u;
+    return a.T <= kWaveTree ? (uint32_t)(own >> (t > tc ? 32 : 0))
+                            : a.bits[((size_t)b * a.T + i) * a.W + (t - tc)];
   };
   uint32_t next = 0u;
   if (t0 < t1) {
@@ -441,8 +448,8 @@ hipError_t with_cache(int d, bool q8, F&& f) {
 Args make_args(const FlashShape& s, const FlashIn& in, const char* ws, const FlashPlan& p,
                float scale) {
   return Args{(const float*)in.q, in.kc, in.vc, in.ks, in.vs, (const float*)in.kn,
-              (const float*)in.vn, reinterpret_cast<const uint32_t*>(ws + p.off_bits), s.Hq, s.Hkv,
-              s.G(), s.T, s.M, s.G() * s.T, (s.T + 31) / 32, scale * kLog2e};
+              (const float*)in.vn, in.parents, reinterpret_cast<const uint32_t*>(ws + p.off_bits),
+              s.Hq, s.Hkv, s.G(), s.T, s.M, s.G() * s.T, (s.T + 31) / 32, scale * kLog2e};
 }
 
 }  // namespace
@@ -450,7 +457,7 @@ Args make_args(const FlashShape& s, const FlashIn& in, const char* ws, const Fla
 hipError_t launch_flash_f32(const FlashShape& s, const FlashPlan& p, const FlashIn& in, void* out,
                             float* lse, char* ws, float scale, hipStream_t st) {
   const bool tree = in.parents != nullptr;
-  if (tree) {
+  if (tree && s.T > kWaveTree) {
     const hipError_t e = launch_tree_bits(s, p, in.parents, ws, st);
     if (e != hipSuccess) return e;
   }

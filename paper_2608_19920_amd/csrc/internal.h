@@ -349,6 +349,22 @@ struct FlashPlan {
   size_t off_keys;              // [BH][M] floats, the ranking copy of a chunk step (not a tree's)
   size_t bytes;
 };
+constexpr int kWaveTree = 64;   // nodes of a tree that a wave masks by itself
+// Ancestors of node `lane`, itself among them, as bits: each lane follows its node up by
+// doubling its way. Parents that are not in [-1, node) count as -1.
+__device__ __forceinline__ uint64_t wave_ancestors(const int32_t* parents, int T, int lane) {
+  int up = lane < T ? parents[lane] : -1;
+  if (up < 0 || up >= lane) up = -1;
+  uint64_t mine = 1ull << lane;
+#pragma unroll 1
+  for (int reach = 1; reach < T; reach *= 2) {
+    const uint64_t more = __shfl(mine, up < 0 ? lane : up, 64);
+    const int next = __shfl(up, up < 0 ? lane : up, 64);
+    mine |= more;
+    up = up < 0 ? -1 : next;
+  }
+  return mine;
+}
 constexpr int kMaxFlashSplit = 32, kMaxColumnRanges = 8;
 constexpr int kColumnKeysF32 = 64;   // keys per block of the float32 column sums
 FlashPlan flash_plan(const FlashShape& s, bool tree);
