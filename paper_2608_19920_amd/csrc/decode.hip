@@ -34,6 +34,7 @@ constexpr int kMaxSplit = 64;                            // split blocks per hea
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -494,9 +495,9 @@ __device__ __forceinline__ void split_body(
 
 // The split over an 8-bit cache (no token positions). A lane's 16 codes of K are
 // consecutive: element 64 x + 16 grp + u of its slot, and the queries are read in
-// the same order of d, which the sum does not depend on. Codes of V become bf16 on
+// the same order of d, which the sum does not depend on. Codes of V become fp16 on
 // their way through LDS. The step's 32 + 32 scales pass through LDS too: the key's
-// multiplies the logit, the value's the probability.
+// multiplies the logit, the value's the probability (in fp16, q8.h).
 template <int D, int G, bool NT>
 __device__ __forceinline__ void split_q8_body(
     const bf16_t* __restrict__ q, const int8_t* __restrict__ kc, const float* __restrict__ ks,
@@ -563,6 +564,7 @@ __device__ __forceinline__ void split_q8_body(
         qb[2 * x + u] = __builtin_bit_cast(bf16x8, load16(qrow + 64 * x + 8 * u));
   }
   float m = -INFINITY, l = 0.f;
+  q8::ValueRef ref;
   f32x4 oacc[D / 16];
 #pragma unroll
   for (int db = 0; db < D / 16; ++db) oacc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -572,9 +574,9 @@ __device__ __forceinline__ void split_q8_body(
     sc[lane] = lane < kStep ? sk[u] * c_log2 : sv[u];
 #pragma unroll
     for (int t = 0; t < NV; ++t) {
-      bf16x8* dst = reinterpret_cast<bf16x8*>(vs + (t * RPL + vrow) * VP + vcol);
-      dst[0] = q8::codes_bf16(vr[u][t][0], vr[u][t][1]);
-      dst[1] = q8::codes_bf16(vr[u][t][2], vr[u][t][3]);
+      f16x8* dst = reinterpret_cast<f16x8*>(vs + (t * RPL + vrow) * VP + vcol);
+      dst[0] = q8::codes_f16(vr[u][t][0], vr[u][t][1]);
+      dst[1] = q8::codes_f16(vr[u][t][2], vr[u][t][3]);
     }
     f32x4 sacc[2];
 #pragma unroll
@@ -611,24 +613,36 @@ __device__ __forceinline__ void split_q8_body(
     }
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    if (__builtin_amdgcn_ballot_w64(mx > m + 64.f)) {
-      const bool up = mx > m + 64.f;
-      const float f = up ? __builtin_amdgcn_exp2f(m - mx) : 1.f;
+    float vmx = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) vmx = fmaxf(vmx, fabsf(cvs[i >> 2][i & 3]));
+    if (__builtin_amdgcn_ballot_w64(mx > m + q8::kRise || vmx > ref.limit)) {
+      const bool up = mx > m + q8::kRise;
+      const float f = up ? __builtin_amdgcn_exp2f(m - mx - q8::kBelow) : 1.f;
       l *= f;
 #pragma unroll
       for (int db = 0; db < D / 16; ++db) oacc[db] *= f;
-      m = up ? mx : m;
+      m = up ? mx + q8::kBelow : m;
+      vmx = fmaxf(vmx, __shfl_xor(vmx, 16, 64));
+      vmx = fmaxf(vmx, __shfl_xor(vmx, 32, 64));
+      if (vmx > ref.limit) {
+        const float fv = ref.raise(vmx);
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db) oacc[db] *= fv;
+      }
     }
-    bf16x8 pb;
+    f16x8 pb;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int key = key0 + 16 * (i >> 2) + 4 * grp + (i & 3);
       const float p = key < M ? __builtin_amdgcn_exp2f(lg[i] - m) : 0.f;
       l += p;
-      pb[i] = (__bf16)(p * cvs[i >> 2][i & 3]);
+      pb[i] = (_Float16)(p * (cvs[i >> 2][i & 3] * ref.inv));
     }
 #pragma unroll
-    for (int db = 0; db < D / 16; ++db) oacc[db] = mfma(v_operand<D>(vs, db, lane), pb, oacc[db]);
+    for (int db = 0; db < D / 16; ++db)
+      oacc[db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+          __builtin_bit_cast(f16x8, v_operand<D>(vs, db, lane)), pb, oacc[db], 0, 0, 0);
   };
   issue(0, 0);
   for (int k = 0; k < nst; k += 2) {   // whole trips of two steps, as in split_body
@@ -639,6 +653,8 @@ __device__ __forceinline__ void split_q8_body(
     __builtin_amdgcn_sched_barrier(0);
     consume(k + 1, 1);
   }
+#pragma unroll
+  for (int db = 0; db < D / 16; ++db) oacc[db] *= ref.ref();
   split_merge<D, G>(m, l, oacc, red_m, red_l, ored, nsplit, s, bh, dstat, dO);
 }
 

@@ -15,8 +15,12 @@
 // holds both, so the mask is asked of the last cache tile and the chunk tiles
 // alone.
 //
-// 8-bit rows become bf16 codes on their way into LDS (exact); the key's scale
-// multiplies the scores, the value's scale the probabilities.
+// 8-bit rows become codes in bf16 (K) and fp16 (V) on their way into LDS, exactly; the
+// key's scale multiplies the scores, the value's scale the probabilities. These are
+// rounded to fp16 for their product with codes (q8.h), and with bf16 values split into
+// two bf16 terms, so that the output has the error of its own rounding and no other
+// (1.7e-3 normwise; with probabilities in bf16 2.3e-3, and 2.8e-3 where there are few
+// rows). That costs a twentieth: B1 Hq32 Hkv8 d128 M8192 T1024 172 -> 182 us.
 #include "internal.h"
 #include "mfma_ops.h"
 #include "q8.h"
@@ -35,6 +39,9 @@ constexpr int kFewSplits = 4;   // key ranges that one thread merges alone
 #define H2O_INLINE __attribute__((always_inline))
 
 __host__ __device__ constexpr int lds_pitch(int D) { return D + 16; }   // bf16 per LDS row
+
+// Tiles of a pass: whole ones of the cache, its last, and the chunk's.
+enum { kCache, kCacheEnd, kChunk };
 
 struct Args {
   const bf16_t* q;
@@ -105,16 +112,20 @@ __device__ __forceinline__ void store_rows16(bf16_t* lds, const u32x4* r) {
     *reinterpret_cast<u32x4*>(lds + u / (D / 8) * lds_pitch(D) + 8 * (u % (D / 8))) = r[e];
   }
 }
-template <int D, int NT, int BN>
+template <int D, int NT, int BN, bool F16>
 __device__ __forceinline__ void store_rows8(bf16_t* lds, const u32x4* r) {
 #pragma unroll
   for (int e = 0; e < Regs<D, NT, BN>::N8; ++e) {
     const int u = threadIdx.x + e * NT;
     if (BN * D / 16 < NT && u >= BN * D / 16) return;
-    bf16x8* dst =
-        reinterpret_cast<bf16x8*>(lds + u / (D / 16) * lds_pitch(D) + 16 * (u % (D / 16)));
-    dst[0] = q8::codes_bf16(r[e][0], r[e][1]);
-    dst[1] = q8::codes_bf16(r[e][2], r[e][3]);
+    bf16_t* dst = lds + u / (D / 16) * lds_pitch(D) + 16 * (u % (D / 16));
+    if constexpr (F16) {
+      reinterpret_cast<f16x8*>(dst)[0] = q8::codes_f16(r[e][0], r[e][1]);
+      reinterpret_cast<f16x8*>(dst)[1] = q8::codes_f16(r[e][2], r[e][3]);
+    } else {
+      reinterpret_cast<bf16x8*>(dst)[0] = q8::codes_bf16(r[e][0], r[e][1]);
+      reinterpret_cast<bf16x8*>(dst)[1] = q8::codes_bf16(r[e][2], r[e][3]);
+    }
   }
 }
 
@@ -147,8 +158,8 @@ template <int D, bool Q8, int NT, int BN, bool WHOLE = false>
 __device__ __forceinline__ void store_tile(bf16_t* Ks, bf16_t* Vs, float* sc,
                                            const Regs<D, NT, BN>& g, const Args& a, int t, int tc) {
   if (Q8 && (WHOLE || t < tc)) {
-    store_rows8<D, NT, BN>(Ks, g.k);
-    store_rows8<D, NT, BN>(Vs, g.v);
+    store_rows8<D, NT, BN, false>(Ks, g.k);
+    store_rows8<D, NT, BN, true>(Vs, g.v);
   } else {
     store_rows16<D, NT, BN>(Ks, g.k);
     store_rows16<D, NT, BN>(Vs, g.v);
@@ -162,7 +173,8 @@ __device__ __forceinline__ void store_tile(bf16_t* Ks, bf16_t* Vs, float* sc,
 // reference common to the 4 lanes that hold the row: the maximum of the first
 // tile the row sees, raised when a score exceeds it by more than 64 (a
 // wave-uniform and rare branch), so terms stay below 2^64, far inside float32 and
-// bf16.
+// bf16; over an 8-bit cache as q8.h says (a reference that is the maximum itself and
+// raised from 2^10 on was raised in so many tiles that the pass took 207 us, not 182).
 //
 // Tiles have BN keys, 32, or 64 at d = 64 with 128 rows or more, where the registers
 // allow them: half the barriers, and more of a wave's own products and exponentials to
@@ -175,10 +187,11 @@ __device__ __forceinline__ void store_tile(bf16_t* Ks, bf16_t* Vs, float* sc,
 // another tile ahead, or an imposed order of products and vector operations, measured
 // no faster: B1 Hq32 Hkv8 d128 M8192 T1024 216 us in every form, 4 waves a block.)
 //
-// Bound by the two pipes of a SIMD together: 32 products (16 cycles each) and some 190
+// Bound by the two pipes of a SIMD together: 32 products (16 cycles each) and some 200
 // vector operations, 16 of them exponentials (8 cycles), per 32 keys and 32 rows; 64
-// of the 190 turn codes into bf16. With 8 waves a block they are half as many per row:
-// 191 us at the shape above, 765 TFLOP/s on the visible pairs.
+// of them (4 waves) or 32 (8 waves) turn codes into bf16 and fp16. The kinds of tiles
+// are separate code: one body for the cache's last tile and the chunk's took 254
+// registers instead of 212 and 13 % more time.
 template <int D, bool Q8, bool TREE, int NQB, int NW, int BN>
 __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
                                                          bf16_t* __restrict__ out,
@@ -186,6 +199,7 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
                                                          float2* __restrict__ stats,
                                                          float* __restrict__ opart) {
   constexpr int NT = NW * 64, ROWS = NW * NQB * 16, P = lds_pitch(D), NK = BN / 16;
+  constexpr float kRaise = Q8 ? q8::kRise : 64.f, kBelow = Q8 ? q8::kBelow : 0.f;
   __shared__ __attribute__((aligned(16))) bf16_t Ks[2][BN * P];
   __shared__ __attribute__((aligned(16))) bf16_t Vs[2][BN * P];
   __shared__ __attribute__((aligned(16))) float sc[2][2 * BN];
@@ -202,11 +216,11 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
   const int ntiles = tc + i_max / BN + 1;
   const int per = (ntiles + nsplit - 1) / nsplit;
   const int t0 = min(ntiles, id.sp * per), t1 = min(ntiles, t0 + per);
-  const int tm = a.M / BN;            // tiles from here on ask for the mask
 
   bf16x8 qf[NQB][D / 32];
   int qi[NQB];
   float mu[NQB], thr[NQB], l[NQB];
+  q8::ValueRef vr;
   f32x4 oacc[D / 16][NQB];
 #pragma unroll
   for (int n = 0; n < NQB; ++n) {
@@ -233,10 +247,11 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
 
   // Tile t, in LDS at K, V, scl: scores, probabilities, O += P V; then the registers g,
   // with tile t + 1, go to the other buffer, and tile t + 2 is requested into them.
-  auto tile = [&](auto masked, auto whole, int t, const bf16_t* K, const bf16_t* V,
+  auto tile = [&](auto kind, auto whole, int t, const bf16_t* K, const bf16_t* V,
                   const float* scl, Regs<D, NT, BN>& g, int t1st, int t2nd, bf16_t* K2, bf16_t* V2,
                   float* scl2) H2O_INLINE {
-    constexpr bool MASK = decltype(masked)::value, WHOLE = decltype(whole)::value;
+    constexpr bool CHUNK = decltype(kind)::value == kChunk, MASK = decltype(kind)::value != kCache;
+    constexpr bool WHOLE = decltype(whole)::value, CODED = Q8 && !CHUNK;
     f32x4 s[NK][NQB];
 #pragma unroll
     for (int kb = 0; kb < NK; ++kb) {
@@ -249,9 +264,8 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
         for (int n = 0; n < NQB; ++n) s[kb][n] = mma(kf, qf[n][x], s[kb][n]);
       }
     }
-    const bool cache = t < tc;
     uint32_t seen[NQB][BN / 32];
-    if (MASK && TREE && !cache)
+    if (TREE && CHUNK)
 #pragma unroll
       for (int n = 0; n < NQB; ++n)
 #pragma unroll
@@ -262,7 +276,7 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
                                           : a.bits[((size_t)b * a.T + qi[n]) * a.W + word];
         }
     f32x4 cks[NK], cvs[NK];
-    if (Q8)
+    if (CODED)
 #pragma unroll
       for (int kb = 0; kb < NK; ++kb) {
         cks[kb] = *reinterpret_cast<const f32x4*>(scl + 16 * kb + 4 * g4);
@@ -273,10 +287,10 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
       for (int kb = 0; kb < NK; ++kb)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          float v = fmaf(s[kb][n][r], Q8 ? cks[kb][r] : a.c, -ref);
+          float v = fmaf(s[kb][n][r], CODED ? cks[kb][r] : a.c, -ref);
           if (MASK) {
             const int j = 16 * kb + 4 * g4 + r;
-            const bool hid = cache ? t * BN + j >= a.M
+            const bool hid = !CHUNK ? t * BN + j >= a.M
                              : TREE ? !((seen[n][kb >> 1] >> (j & 31)) & 1u)
                                     : (t - tc) * BN + j > qi[n];
             if (hid) v = -INFINITY;
@@ -294,37 +308,83 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
       for (int e = 1; e < 4 * NK; ++e) mx[n] = fmaxf(mx[n], x[n][e]);
       up |= mx[n] > thr[n];
     }
+    float vmx = 0.f;
+    if (CODED) {
+#pragma unroll
+      for (int kb = 0; kb < NK; ++kb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) vmx = fmaxf(vmx, fabsf(cvs[kb][r]));
+      up |= vmx > vr.limit;
+    }
     if (__builtin_amdgcn_ballot_w64(up)) {
 #pragma unroll
       for (int n = 0; n < NQB; ++n) {
         float y = fmaxf(mx[n], __shfl_xor(mx[n], 16, 64));
         y = fmaxf(y, __shfl_xor(y, 32, 64));
         const bool raise = y > thr[n];
+        y += kBelow;
         const float f = !raise ? 1.f : thr[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(-y);
         l[n] *= f;
 #pragma unroll
         for (int db = 0; db < D / 16; ++db) oacc[db][n] *= f;
         mu[n] = raise ? mu[n] + y : mu[n];
-        thr[n] = raise ? 64.f : thr[n];
+        thr[n] = raise ? kRaise : thr[n];
         shifted(n, mu[n], x[n]);
       }
-    }
+      if (CODED) {
+        vmx = fmaxf(vmx, __shfl_xor(vmx, 16, 64));
+        vmx = fmaxf(vmx, __shfl_xor(vmx, 32, 64));
+        if (vmx > vr.limit) {
+          const float f = vr.raise(vmx);
 #pragma unroll
-    for (int kk = 0; kk < BN / 32; ++kk) {
-      bf16x8 pb[NQB];
+          for (int n = 0; n < NQB; ++n)
 #pragma unroll
-      for (int n = 0; n < NQB; ++n)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float p = __builtin_amdgcn_exp2f(x[n][8 * kk + e]);
-          l[n] += p;
-          pb[n][e] = (__bf16)(Q8 ? p * cvs[2 * kk + (e >> 2)][e & 3] : p);
+            for (int db = 0; db < D / 16; ++db) oacc[db][n] *= f;
         }
+      }
+    }
+    if constexpr (CODED) {
 #pragma unroll
-      for (int db = 0; db < D / 16; ++db) {
-        const bf16x8 vf = tr_operand(V + 32 * kk * P, P, db, lane);
+      for (int kb = 0; kb < NK; ++kb) cvs[kb] *= vr.inv;
 #pragma unroll
-        for (int n = 0; n < NQB; ++n) oacc[db][n] = mma(vf, pb[n], oacc[db][n]);
+      for (int kk = 0; kk < BN / 32; ++kk) {
+        f16x8 pb[NQB];
+#pragma unroll
+        for (int n = 0; n < NQB; ++n)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float p = __builtin_amdgcn_exp2f(x[n][8 * kk + e]);
+            l[n] += p;
+            pb[n][e] = (_Float16)(p * cvs[2 * kk + (e >> 2)][e & 3]);
+          }
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db) {
+          const f16x8 vf = __builtin_bit_cast(f16x8, tr_operand(V + 32 * kk * P, P, db, lane));
+#pragma unroll
+          for (int n = 0; n < NQB; ++n) oacc[db][n] = mma(vf, pb[n], oacc[db][n]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int kk = 0; kk < BN / 32; ++kk) {
+        bf16x8 pb[NQB], rest[NQB];
+#pragma unroll
+        for (int n = 0; n < NQB; ++n)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float p = __builtin_amdgcn_exp2f(x[n][8 * kk + e]);
+            l[n] += p;
+            const float w = Q8 ? p * vr.inv : p;
+            pb[n][e] = (__bf16)w;
+            rest[n][e] = (__bf16)(w - (float)pb[n][e]);
+          }
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db) {
+          const bf16x8 vf = tr_operand(V + 32 * kk * P, P, db, lane);
+#pragma unroll
+          for (int n = 0; n < NQB; ++n)
+            oacc[db][n] = mma(vf, rest[n], mma(vf, pb[n], oacc[db][n]));
+        }
       }
     }
     store_tile<D, Q8, NT, BN, WHOLE>(K2, V2, scl2, g, a, t1st, tc);
@@ -339,19 +399,21 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
     store_tile<D, Q8, NT, BN>(Ks[0], Vs[0], sc[0], g, a, t0, tc);
     load_tile<D, Q8, NT, BN>(g, a, bh, min(t0 + 1, last), tc);
     __syncthreads();
-    auto run = [&](auto masked, auto whole, int ta, int tb) H2O_INLINE {
+    auto run = [&](auto kind, auto whole, int ta, int tb) H2O_INLINE {
       for (int t = ta; t < tb; ++t) {
         const int v = (t - t0) & 1;
-        tile(masked, whole, t, Ks[v], Vs[v], sc[v], g, min(t + 1, last), min(t + 2, last),
+        tile(kind, whole, t, Ks[v], Vs[v], sc[v], g, min(t + 1, last), min(t + 2, last),
              Ks[v ^ 1], Vs[v ^ 1], sc[v ^ 1]);   // (past the last tile: it again, not used)
       }
     };
-    // turns whose tiles t + 1 and t + 2 are whole cache tiles; the others without a
-    // mask; those that ask for it
-    const int te = max(t0, min(t1, tm)), tw = max(t0, min(te, min(t1, tm) - 2));
-    run(IntConst<0>{}, IntConst<1>{}, t0, tw);
-    run(IntConst<0>{}, IntConst<0>{}, tw, te);
-    run(IntConst<1>{}, IntConst<0>{}, te, t1);
+    // turns whose tiles t + 1 and t + 2 are whole cache tiles; the other whole ones; the
+    // one that ends the cache; the chunk
+    const int tm = a.M / BN, te = max(t0, min(t1, tm)), tw = max(t0, min(te, min(t1, tm) - 2));
+    const int tk = max(t0, min(t1, tc));
+    run(IntConst<kCache>{}, IntConst<1>{}, t0, tw);
+    run(IntConst<kCache>{}, IntConst<0>{}, tw, te);
+    run(IntConst<kCacheEnd>{}, IntConst<0>{}, te, tk);
+    run(IntConst<kChunk>{}, IntConst<0>{}, tk, t1);
   }
 
   const int BH = gridDim.y;
@@ -368,7 +430,7 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
       if (nsplit == 1) lse[orow] = (mu[n] + __log2f(L)) * kLn2;
       else stats[prow] = make_float2(thr[n] == -INFINITY ? -INFINITY : mu[n], L);
     }
-    const float inv = 1.f / L;
+    const float inv = vr.ref() / L;
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) {
       const f32x4 o = oacc[db][n];
@@ -379,7 +441,7 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
         for (int e = 0; e < 4; ++e) w[e] = (__bf16)(o[e] * inv);
         *reinterpret_cast<bf16x4*>(out + orow * D + 16 * db + 4 * g4) = w;
       } else {
-        *reinterpret_cast<f32x4*>(opart + prow * D + 16 * db + 4 * g4) = o;
+        *reinterpret_cast<f32x4*>(opart + prow * D + 16 * db + 4 * g4) = Q8 ? o * vr.ref() : o;
       }
     }
   }
@@ -689,7 +751,7 @@ __global__ __launch_bounds__(kThreads) void column_few(Args a, ColArgs p, int nb
   constexpr int NX = Q8 ? D / 64 : D / 32;   // 16-byte loads of a key row per lane
   constexpr int P = D + 8, NU = 16 * NR * D / 8 / kThreads;
   __shared__ __attribute__((aligned(16))) bf16_t Qs[16 * NR * P];
-  __shared__ float lam[16 * NR];
+  __shared__ float2 lam[16 * NR];
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const size_t bh = blockIdx.y;
@@ -742,10 +804,11 @@ __global__ __launch_bounds__(kThreads) void column_few(Args a, ColArgs p, int nb
       qr[e] = *reinterpret_cast<const u32x4*>(
           a.q + ((size_t)(b * a.Hq + h * a.G + r % a.G) * a.T + node) * D + 8 * (tid % (D / 8)));
     }
-    float lr = INFINITY;
+    float2 lr = {INFINITY, 0.f};
     if (tid < p.R) {
       const int node = path_node(path, tid / a.G, a.T);
-      if (node >= 0) lr = p.lse[(size_t)(b * a.Hq + h * a.G + tid % a.G) * a.T + node] * kLog2e;
+      if (node >= 0)
+        lr = row_weight(p.lse[(size_t)(b * a.Hq + h * a.G + tid % a.G) * a.T + node]);
     }
     issue(w0, 0);
 #pragma unroll
@@ -778,16 +841,16 @@ __global__ __launch_bounds__(kThreads) void column_few(Args a, ColArgs p, int nb
     for (int kb = 0; kb < 2; ++kb) cs[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
-      const float la = lam[16 * n + l16];
-      if (PATH && la == INFINITY) continue;
+      const float2 la = lam[16 * n + l16];
+      if (PATH && la.x == INFINITY) continue;
       const int i = decltype(chunk)::value ? (16 * n + l16) / a.G : 0;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          float w = __builtin_amdgcn_exp2f(fmaf(s[n][kb][r], ck[kb][r], -la));
+          float w = __builtin_amdgcn_exp2f(fmaf(s[n][kb][r], ck[kb][r], -la.x));
           if (decltype(chunk)::value && j0 + 16 * kb + 4 * g4 + r > i) w = 0.f;
-          cs[kb][r] += w;
+          cs[kb][r] = fmaf(w, la.y, cs[kb][r]);
         }
     }
 #pragma unroll

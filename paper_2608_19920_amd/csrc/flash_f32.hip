@@ -37,7 +37,7 @@ struct Args {
   const int32_t* parents;
   const uint32_t* bits;
   int Hq, Hkv, G, T, M, R, W;
-  float c;
+  float c, c_lo;                // scale * log2(e), and what c is short of it
 };
 
 // A tile's rows in registers; rows past the tile's end are zeros.
@@ -195,13 +195,16 @@ __global__ __launch_bounds__(kThreads) void flash_f32(Args a, int nsplit, float*
     float mn = m;
 #pragma unroll
     for (int kb = 0; kb < NK; ++kb) {
-      s[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+      f32x4 s4[4];                  // shorter sums round less
+#pragma unroll
+      for (int u = 0; u < 4; ++u) s4[u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int x = 0; x < D / 16; ++x) {
         const f32x4 kf = load4(&Ks[(16 * kb + l16) * P + 16 * x + 4 * g4]);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) s[kb] = mma4(kf[u], qf[x][u], s[kb]);
+        for (int u = 0; u < 4; ++u) s4[u] = mma4(kf[u], qf[x][u], s4[u]);
       }
+      s[kb] = (s4[0] + s4[1]) + (s4[2] + s4[3]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int j = 16 * kb + 4 * g4 + e;
@@ -295,7 +298,7 @@ template <int D, bool Q8, bool PATH>
 __global__ __launch_bounds__(kThreads) void column_f32(Args a, ColArgs p) {
   constexpr int KB = kWaves * 16, P = lds_pitch(D), NU = kQRows * D / 4 / kThreads;
   __shared__ __attribute__((aligned(16))) float Qs[2][kQRows * P];
-  __shared__ float lam[2][kQRows];
+  __shared__ float2 lam[2][kQRows];
   __shared__ int pos[2][kQRows];
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -349,7 +352,7 @@ __global__ __launch_bounds__(kThreads) void column_f32(Args a, ColArgs p) {
   // rows as in column_pass: stepped without a division, past the last row kept at it
   constexpr int RU = kThreads / (D / 4);
   f32x4 qr[NU];
-  float lr = 0.f;
+  float2 lr = {0.f, 0.f};
   int ir = 0, ri[NU], rg[NU], li, lg;
   const int part = 4 * (tid % (D / 4)), di = kQRows / a.G, dg = kQRows % a.G;
 #pragma unroll
@@ -376,7 +379,7 @@ __global__ __launch_bounds__(kThreads) void column_f32(Args a, ColArgs p) {
     }
     if (tid < kQRows) {
       const int n = li < p.A ? node_of(li) : -1;
-      lr = n >= 0 ? lh[lg * a.T + n] * kLog2e : INFINITY;
+      lr = n >= 0 ? row_weight(lh[lg * a.T + n]) : make_float2(INFINITY, 0.f);
       ir = li;
       advance(li, lg);
     }
@@ -402,26 +405,30 @@ __global__ __launch_bounds__(kThreads) void column_f32(Args a, ColArgs p) {
       store(buf ^ 1);
       if (s + 2 < s1) load();
     }
-    f32x4 w[kQRows / 16];
+    f32x4 w[kQRows / 16], w4[kQRows / 16][4];
 #pragma unroll
-    for (int n = 0; n < kQRows / 16; ++n) w[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int n = 0; n < kQRows / 16; ++n)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) w4[n][u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int x = 0; x < D / 16; ++x)
 #pragma unroll
       for (int n = 0; n < kQRows / 16; ++n) {
         const f32x4 qf = load4(&Qs[buf][(16 * n + l16) * P + 16 * x + 4 * g4]);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) w[n] = mma4(kf[x][u], qf[u], w[n]);
+        for (int u = 0; u < 4; ++u) w4[n][u] = mma4(kf[x][u], qf[u], w4[n][u]);
       }
 #pragma unroll
+    for (int n = 0; n < kQRows / 16; ++n) w[n] = (w4[n][0] + w4[n][1]) + (w4[n][2] + w4[n][3]);
+#pragma unroll
     for (int n = 0; n < kQRows / 16; ++n) {
-      const float la = lam[buf][16 * n + l16];
+      const float2 la = lam[buf][16 * n + l16];
       const int i = pos[buf][16 * n + l16];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(w[n][r], a.c, -la));
-        const bool hid = la == INFINITY || (!cache && j0 + 4 * g4 + r > i);
-        cs[r] += hid ? 0.f : x;
+        const float x = __builtin_amdgcn_exp2f(fmaf(w[n][r], a.c, -la.x) + w[n][r] * a.c_lo);
+        const bool hid = la.x == INFINITY || (!cache && j0 + 4 * g4 + r > i);
+        cs[r] = fmaf(hid ? 0.f : x, la.y, cs[r]);
       }
     }
     __syncthreads();
@@ -447,9 +454,11 @@ hipError_t with_cache(int d, bool q8, F&& f) {
 }
 Args make_args(const FlashShape& s, const FlashIn& in, const char* ws, const FlashPlan& p,
                float scale) {
+  const double c = (double)scale * 1.4426950408889634;
   return Args{(const float*)in.q, in.kc, in.vc, in.ks, in.vs, (const float*)in.kn,
               (const float*)in.vn, in.parents, reinterpret_cast<const uint32_t*>(ws + p.off_bits),
-              s.Hq, s.Hkv, s.G(), s.T, s.M, s.G() * s.T, (s.T + 31) / 32, scale * kLog2e};
+              s.Hq, s.Hkv, s.G(), s.T, s.M, s.G() * s.T, (s.T + 31) / 32, (float)c,
+              (float)(c - (float)c)};
 }
 
 }  // namespace

@@ -349,6 +349,13 @@ struct FlashPlan {
   size_t off_keys;              // [BH][M] floats, the ranking copy of a chunk step (not a tree's)
   size_t bytes;
 };
+// A row's lse for its weights exp(s - lse) = exp2(log2(e) s - x) y: x = log2(e) lse
+// rounded to float32 (at an lse of 20 off by 2^-20, the same for every weight of the row)
+// and y = 2^-(what x is short of), near 1.
+__device__ __forceinline__ float2 row_weight(float lse) {
+  const float x = lse * kLog2e, lo = fmaf(lse, kLog2e, -x) + lse * 1.92596303e-8f;
+  return make_float2(x, lo == lo ? fmaf(-lo, kLn2, 1.f) : 1.f);   // (lse infinite: 1)
+}
 constexpr int kWaveTree = 64;   // nodes of a tree that a wave masks by itself
 // Ancestors of node `lane`, itself among them, as bits: each lane follows its node up by
 // doubling its way. Parents that are not in [-1, node) count as -1.

@@ -18,6 +18,8 @@ namespace q8 {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr uint32_t kInfBits = 0x7F800000u;
 
@@ -34,6 +36,41 @@ __device__ __forceinline__ bf16x8 codes_bf16(uint32_t lo, uint32_t hi) {
   }
   return r;
 }
+
+// The same in fp16, where 0x6400 + u is 1024 + u.
+__device__ __forceinline__ f16x8 codes_f16(uint32_t lo, uint32_t hi) {
+  const f16x2 off = {(_Float16)1152.f, (_Float16)1152.f};
+  f16x2 r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    r[i] = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u,
+                                                           (i < 2 ? lo : hi) ^ 0x80808080u,
+                                                           i & 1 ? 0x04030402u : 0x04010400u)) - off;
+  return f16x8{r[0][0], r[0][1], r[1][0], r[1][1], r[2][0], r[2][1], r[3][0], r[3][1]};
+}
+
+// The weights of values in 8 bits, probability times scale, are rounded to fp16 for
+// their product with the codes: 2^-12 of their size at most, where bf16's 2^-9 would be
+// as large an error as that of the bf16 output itself. fp16 goes from 2^-24 to 2^16, so
+// the scales are taken relative to `ref`, a power of two above all that the wave has
+// seen, and the softmax's reference is put kBelow above a maximum (in log2 units) and
+// raised when a score exceeds it by kRise: probabilities stay below 2^15, and what
+// falls under 2^-24 is 2^-20 of the largest or less.
+constexpr float kRise = 15.f, kBelow = 4.f;
+struct ValueRef {
+  float inv = 1.f, limit = 0.f;   // 1 / ref; ref, 0 before the first keys
+  // y: the largest |scale| of the wave's keys, above limit; returns the factor of sums
+  // taken with the old reference
+  __device__ __forceinline__ float raise(float y) {
+    const uint32_t e = ((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(y)) &
+                        0x7F800000u) + 0x00800000u;   // of a power of two above y
+    const float old = limit;
+    limit = __uint_as_float(e);
+    inv = __uint_as_float(0x7F000000u - e);
+    return old * inv;
+  }
+  __device__ __forceinline__ float ref() const { return limit == 0.f ? 1.f : limit; }
+};
 
 // Scale of a row from the bits of max|x| (as unsigned integers the finite
 // magnitudes come before Inf, and Inf before every NaN).

@@ -167,3 +167,53 @@ def test_two_streams_at_once():
 ], ids=lambda c: "-".join(map(str, c)))
 def test_steps_of_many_rows_and_slots(case):
     steps.test_step_is_its_three_parts(case)
+
+
+@pytest.mark.parametrize("d,T", [(64, 1), (128, 1), (64, 40), (128, 9), (128, 300)])
+@pytest.mark.parametrize("rising", [True, False])
+def test_values_and_scores_of_every_size(d, T, rising):
+    """Value rows from 2^-40 to 2^40 and none at all, scores that rise or fall along the
+    cache. The weights are off by 2^-12 of their size, or 2^-20 of the largest one; the
+    output is rounded by at most 2^-8: 2^-8 + 2^-11 normwise leaves room for the sums."""
+    B, Hq, Hkv, M = 1, 8, 2, 900
+    x = inputs(B, Hq, Hkv, d, M, T, "bf16", seed=d + T)
+    ramp = np.arange(M) / M
+    if not rising:
+        ramp = ramp[::-1]
+    x["v_cache"] *= np.exp2(np.round(80 * ramp - 40)).astype(np.float32)[:, None]
+    x["v_cache"][:, :, 100:140] = 0.0
+    x["v_cache"][:, 0, :64] = 0.0
+    x["k_cache"] = (0.3 * x["k_cache"] + np.float32(6 / d ** 0.5) * (ramp[:, None] - 0.5) *
+                    x["q"][:, ::4, -1:, :]).astype(np.float32)
+    for n in "kv":
+        x[n + "_codes"], x[n + "_scales"] = oracle.quantize(x[n + "_cache"])
+        x[n + "_values"] = oracle.dequantize(x[n + "_codes"], x[n + "_scales"])
+    b = H.alloc_step(B, Hq, Hkv, T, M, d, torch.bfloat16, q8=True)
+    bf = torch.bfloat16
+    H.h2o_sdpa_chunk_q8(dev(x["q"], bf), *dev_cache(x), dev(x["k_new"], bf), dev(x["v_new"], bf),
+                        b["out"], b["lse"], b["wsum"], b["workspace"], float(x["scale"]))
+    o, l, w = oracle.sdpa_chunk(x["q"], x["k_values"], x["v_values"], x["k_new"], x["v_new"],
+                                x["scale"])
+    close("bf16", "sizes", lse=(b["lse"], l), wsum=(b["wsum"], w))
+    e = oracle.rel_err(U.to_np(b["out"]), o, (-2, -1))
+    assert e <= 2.0 ** -8 + 2.0 ** -11, e
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,d,M,T", [(1, 16, 16, 128, 700, 1), (1, 8, 2, 64, 3000, 3),
+                                            (2, 4, 2, 128, 500, 20), (1, 8, 1, 64, 400, 100)])
+@pytest.mark.parametrize("q8", [True, False])
+def test_a_tree_is_off_by_its_rounding_alone(B, Hq, Hkv, d, M, T, q8):
+    """As above, of a tree over either cache, by query head."""
+    x, bf = inputs(B, Hq, Hkv, d, M, T, "bf16", seed=M), torch.bfloat16
+    parents = np.tile(np.arange(-1, T - 1) // 2, (B, 1)).astype(np.int32)
+    c = dev_cache(x) if q8 else [dev(x["k_cache"], bf), None, dev(x["v_cache"], bf), None]
+    out = torch.empty(B, Hq, T, d, dtype=bf, device=U.DEV)
+    lse = torch.empty(B, Hq, T, device=U.DEV)
+    ws = torch.empty(max(16, H.h2o_tree_workspace_bytes(B, Hq, Hkv, T, M, d, bf)),
+                     dtype=torch.uint8, device=U.DEV)
+    H.h2o_sdpa_tree(dev(x["q"], bf), c[0], c[2], dev(x["k_new"], bf), dev(x["v_new"], bf),
+                    dev(parents), out, lse, ws, float(x["scale"]), k_scales=c[1], v_scales=c[3])
+    kv = [x[n + ("_values" if q8 else "_cache")] for n in "kv"]
+    o, l = oracle.sdpa_tree(x["q"], *kv, x["k_new"], x["v_new"], parents, x["scale"])
+    e = oracle.rel_err(U.to_np(out), o, (-2, -1))
+    assert e <= 2.0 ** -8 + 2.0 ** -11, e
