@@ -5,8 +5,8 @@
 //
 // A row whose scale would be subnormal has scale 0 and codes 0; a row with an Inf
 // or NaN has scale NaN and codes 0, so it reads back as NaN and never as data.
-// A code is exact in bf16 (7 bits), so a matrix product over codes is as exact as
-// one over bf16 data; the scale of a key multiplies its column of scores, the
+// A code is exact in bf16 and fp16 (7 bits), so a matrix product over codes is as exact
+// as one over bf16 data; the scale of a key multiplies its column of scores, the
 // scale of a value its column of probabilities, both in float32.
 #pragma once
 
