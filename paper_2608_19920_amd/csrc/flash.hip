@@ -151,7 +151,6 @@ __device__ __forceinline__ void load_tile(Regs<D, NT, BN>& g, const Args& a, siz
     const size_t row = bh * (size_t)a.T + j0;
     load_rows16<D, NT, BN>(g.k, a.kn + row * D, n);
     load_rows16<D, NT, BN>(g.v, a.vn + row * D, n);
-    if (Q8) g.s = 1.f;
   }
 }
 template <int D, bool Q8, int NT, int BN, bool WHOLE = false>
@@ -160,11 +159,11 @@ __device__ __forceinline__ void store_tile(bf16_t* Ks, bf16_t* Vs, float* sc,
   if (Q8 && (WHOLE || t < tc)) {
     store_rows8<D, NT, BN, false>(Ks, g.k);
     store_rows8<D, NT, BN, true>(Vs, g.v);
+    if (threadIdx.x < 2 * BN) sc[threadIdx.x] = threadIdx.x < BN ? g.s * a.c : g.s;
   } else {
     store_rows16<D, NT, BN>(Ks, g.k);
     store_rows16<D, NT, BN>(Vs, g.v);
   }
-  if (Q8 && threadIdx.x < 2 * BN) sc[threadIdx.x] = threadIdx.x < BN ? g.s * a.c : g.s;
 }
 
 // --------------------------------------------------------------------- flash
