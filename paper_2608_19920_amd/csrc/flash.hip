@@ -412,6 +412,15 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
     run(IntConst<kCache>{}, IntConst<1>{}, t0, tw);
     run(IntConst<kCache>{}, IntConst<0>{}, tw, te);
     run(IntConst<kCacheEnd>{}, IntConst<0>{}, te, tk);
+    // the chunk's values are of any size, whatever the cache's: probabilities relative to
+    // a far smaller reference would leave float32
+    if (Q8 && tk < t1 && vr.limit < 1.f) {
+      const float f = vr.raise(0.5f);   // to 1
+#pragma unroll
+      for (int n = 0; n < NQB; ++n)
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db) oacc[db][n] *= f;
+    }
     run(IntConst<kChunk>{}, IntConst<0>{}, tk, t1);
   }
 
