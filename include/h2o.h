@@ -373,8 +373,11 @@ size_t h2o_q8_workspace_bytes(int B, int Hq, int Hkv, int T, int M, int d,
                               int dtype, int policy);
 
 /* h2o_sdpa_chunk over an 8-bit cache: the results are those of the attention over
- * the values that the codes stand for, without rounding these to dtype (the
- * scales enter the scores and the probabilities in float32). The chunk's own
+ * the values that the codes stand for, without rounding these to dtype: the scales
+ * enter the scores in float32 and, with dtype H2O_F32, everything else. With
+ * H2O_BF16 the products of a probability and a value's scale are rounded to fp16
+ * (2^-11 of their size, small ones 2^-11 of the row's largest together), and values
+ * 2^70 or more below the largest ones of their KV head may count as 0. The chunk's own
  * keys and values are in dtype. M may be 0 (the cache pointers may be NULL then). */
 int h2o_sdpa_chunk_q8(const void* q, const int8_t* k_codes, const float* k_scales,
                       const int8_t* v_codes, const float* v_scales,

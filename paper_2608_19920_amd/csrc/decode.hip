@@ -497,7 +497,7 @@ __device__ __forceinline__ void split_body(
 // consecutive: element 64 x + 16 grp + u of its slot, and the queries are read in
 // the same order of d, which the sum does not depend on. Codes of V become fp16 on
 // their way through LDS. The step's 32 + 32 scales pass through LDS too: the key's
-// multiplies the logit, the value's the probability (in fp16, q8.h).
+// multiplies the logit, the value's the probability (in fp16, with m where q8.h puts it).
 template <int D, int G, bool NT>
 __device__ __forceinline__ void split_q8_body(
     const bf16_t* __restrict__ q, const int8_t* __restrict__ kc, const float* __restrict__ ks,
@@ -563,7 +563,8 @@ __device__ __forceinline__ void split_q8_body(
       for (int u = 0; u < 2; ++u)
         qb[2 * x + u] = __builtin_bit_cast(bf16x8, load16(qrow + 64 * x + 8 * u));
   }
-  float m = -INFINITY, l = 0.f;
+  float m = 0.f, l = 0.f, most = -1.f;
+  const float aim = q8::aim_of(nst * kStep);
   q8::ValueRef ref;
   f32x4 oacc[D / 16];
 #pragma unroll
@@ -596,13 +597,13 @@ __device__ __forceinline__ void split_q8_body(
       cks[kb] = *reinterpret_cast<const f32x4*>(sc + 16 * kb + 4 * grp);
       cvs[kb] = *reinterpret_cast<const f32x4*>(sc + kStep + 16 * kb + 4 * grp);
     }
-    float lg[8], mx = -INFINITY;
+    float lg[8], vmx = 0.f;
     const bool tail = key0 + kStep > M;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       lg[i] = sacc[i >> 2][i & 3] * cks[i >> 2][i & 3];
       if (tail && key0 + 16 * (i >> 2) + 4 * grp + (i & 3) >= M) lg[i] = -INFINITY;
-      mx = fmaxf(mx, lg[i]);
+      vmx = fmaxf(vmx, fabsf(cvs[i >> 2][i & 3]));
     }
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
@@ -611,34 +612,44 @@ __device__ __forceinline__ void split_q8_body(
       *reinterpret_cast<f32x4*>(dst) =
           f32x4{lg[4 * kb], lg[4 * kb + 1], lg[4 * kb + 2], lg[4 * kb + 3]};
     }
-    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    float vmx = 0.f;
+    if (__builtin_amdgcn_ballot_w64(vmx > ref.limit)) {
+      const float f = ref.raise(q8::row_max(vmx));
+      most = -1.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) vmx = fmaxf(vmx, fabsf(cvs[i >> 2][i & 3]));
-    if (__builtin_amdgcn_ballot_w64(mx > m + q8::kRise || vmx > ref.limit)) {
-      const bool up = mx > m + q8::kRise;
-      const float f = up ? __builtin_amdgcn_exp2f(m - mx - q8::kBelow) : 1.f;
+      for (int db = 0; db < D / 16; ++db) oacc[db] *= f;
+    }
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) cvs[kb] *= ref.inv;
+    float sum;
+    f16x8 pb;
+    auto weigh = [&]() {   // (slots past M: logits -inf)
+      sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float p = __builtin_amdgcn_exp2f(lg[i] - m);
+        sum += p;
+        pb[i] = (_Float16)(p * cvs[i >> 2][i & 3]);
+      }
+      return q8::largest(pb);
+    };
+    const float top = weigh();
+    if (__builtin_amdgcn_ballot_w64(top >= most || sum >= q8::kSum)) {
+      float y = -INFINITY, yc = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = lg[i] - m, lv = __log2f(fabsf(cvs[i >> 2][i & 3]));
+        y = fmaxf(y, x + lv);
+        yc = fmaxf(yc, x + fmaxf(lv, q8::kLeast));
+      }
+      const bool asks = q8::any_of_row(top >= most || sum >= q8::kSum, col);
+      float f = 1.f;
+      if (asks) f = q8::move(m, most, col, y, yc, l, aim);
       l *= f;
 #pragma unroll
       for (int db = 0; db < D / 16; ++db) oacc[db] *= f;
-      m = up ? mx + q8::kBelow : m;
-      vmx = fmaxf(vmx, __shfl_xor(vmx, 16, 64));
-      vmx = fmaxf(vmx, __shfl_xor(vmx, 32, 64));
-      if (vmx > ref.limit) {
-        const float fv = ref.raise(vmx);
-#pragma unroll
-        for (int db = 0; db < D / 16; ++db) oacc[db] *= fv;
-      }
+      weigh();
     }
-    f16x8 pb;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int key = key0 + 16 * (i >> 2) + 4 * grp + (i & 3);
-      const float p = key < M ? __builtin_amdgcn_exp2f(lg[i] - m) : 0.f;
-      l += p;
-      pb[i] = (_Float16)(p * (cvs[i >> 2][i & 3] * ref.inv));
-    }
+    l += sum;
 #pragma unroll
     for (int db = 0; db < D / 16; ++db)
       oacc[db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
@@ -655,6 +666,7 @@ __device__ __forceinline__ void split_q8_body(
   }
 #pragma unroll
   for (int db = 0; db < D / 16; ++db) oacc[db] *= ref.ref();
+  if (q8::row_max(l) == 0.f) m = -INFINITY;   // a stream without keys
   split_merge<D, G>(m, l, oacc, red_m, red_l, ored, nsplit, s, bh, dstat, dO);
 }
 

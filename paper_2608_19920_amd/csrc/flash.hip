@@ -17,10 +17,13 @@
 //
 // 8-bit rows become codes in bf16 (K) and fp16 (V) on their way into LDS, exactly; the
 // key's scale multiplies the scores, the value's scale the probabilities. These are
-// rounded to fp16 for their product with codes (q8.h), and with bf16 values split into
-// two bf16 terms, so that the output has the error of its own rounding and no other
+// rounded to fp16 for their product with codes, against a reference that goes by the
+// row's weights (q8.h), and with bf16 values split into two bf16 terms, so that next to
+// the rounding of the output theirs is small, whatever the values' and the scores' sizes
 // (1.7e-3 normwise; with probabilities in bf16 2.3e-3, and 2.8e-3 where there are few
-// rows). That costs a twentieth: B1 Hq32 Hkv8 d128 M8192 T1024 172 -> 182 us.
+// rows). B1 Hq32 Hkv8 d128 M8192 T1024: 202 us; with probabilities in bf16 172, with a
+// reference by the scores and the largest scale, which loses rows beside a larger one that
+// nobody attends, 185, with two bf16 terms for codes as well 227.
 #include "internal.h"
 #include "mfma_ops.h"
 #include "q8.h"
@@ -172,8 +175,7 @@ __device__ __forceinline__ void store_tile(bf16_t* Ks, bf16_t* Vs, float* sc,
 // reference common to the 4 lanes that hold the row: the maximum of the first
 // tile the row sees, raised when a score exceeds it by more than 64 (a
 // wave-uniform and rare branch), so terms stay below 2^64, far inside float32 and
-// bf16; over an 8-bit cache as q8.h says (a reference that is the maximum itself and
-// raised from 2^10 on was raised in so many tiles that the pass took 207 us, not 182).
+// bf16; over an 8-bit cache as q8.h says, and 15 in place of 64 in the chunk's tiles.
 //
 // Tiles have BN keys, 32, or 64 at d = 64 with 128 rows or more, where the registers
 // allow them: half the barriers, and more of a wave's own products and exponentials to
@@ -198,7 +200,7 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
                                                          float2* __restrict__ stats,
                                                          float* __restrict__ opart) {
   constexpr int NT = NW * 64, ROWS = NW * NQB * 16, P = lds_pitch(D), NK = BN / 16;
-  constexpr float kRaise = Q8 ? q8::kRise : 64.f, kBelow = Q8 ? q8::kBelow : 0.f;
+  constexpr float kRaise = Q8 ? 15.f : 64.f;
   __shared__ __attribute__((aligned(16))) bf16_t Ks[2][BN * P];
   __shared__ __attribute__((aligned(16))) bf16_t Vs[2][BN * P];
   __shared__ __attribute__((aligned(16))) float sc[2][2 * BN];
@@ -220,6 +222,7 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
   int qi[NQB];
   float mu[NQB], thr[NQB], l[NQB];
   q8::ValueRef vr;
+  float aim = 0.f;
   f32x4 oacc[D / 16][NQB];
 #pragma unroll
   for (int n = 0; n < NQB; ++n) {
@@ -231,7 +234,7 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) qf[n][s] = *reinterpret_cast<const bf16x8*>(src + 32 * s);
     mu[n] = 0.f;
-    thr[n] = -INFINITY;               // no tile seen yet
+    thr[n] = Q8 ? -1.f : -INFINITY;   // no tile seen yet
     l[n] = 0.f;
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) oacc[db][n] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -297,73 +300,105 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
           x[4 * kb + r] = v;
         }
     };
-    float x[NQB][4 * NK], mx[NQB];
-    bool up = false;
-#pragma unroll
-    for (int n = 0; n < NQB; ++n) {
-      shifted(n, mu[n], x[n]);
-      mx[n] = x[n][0];
-#pragma unroll
-      for (int e = 1; e < 4 * NK; ++e) mx[n] = fmaxf(mx[n], x[n][e]);
-      up |= mx[n] > thr[n];
-    }
-    float vmx = 0.f;
-    if (CODED) {
+    if constexpr (CODED) {
+      float vmx = 0.f;
 #pragma unroll
       for (int kb = 0; kb < NK; ++kb)
 #pragma unroll
         for (int r = 0; r < 4; ++r) vmx = fmaxf(vmx, fabsf(cvs[kb][r]));
-      up |= vmx > vr.limit;
-    }
-    if (__builtin_amdgcn_ballot_w64(up)) {
+      if (__builtin_amdgcn_ballot_w64(vmx > vr.limit)) {
+        const float f = vr.raise(q8::row_max(vmx));
 #pragma unroll
-      for (int n = 0; n < NQB; ++n) {
-        float y = fmaxf(mx[n], __shfl_xor(mx[n], 16, 64));
-        y = fmaxf(y, __shfl_xor(y, 32, 64));
-        const bool raise = y > thr[n];
-        y += kBelow;
-        const float f = !raise ? 1.f : thr[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(-y);
-        l[n] *= f;
+        for (int n = 0; n < NQB; ++n) {
+          thr[n] = -1.f;
 #pragma unroll
-        for (int db = 0; db < D / 16; ++db) oacc[db][n] *= f;
-        mu[n] = raise ? mu[n] + y : mu[n];
-        thr[n] = raise ? kRaise : thr[n];
-        shifted(n, mu[n], x[n]);
-      }
-      if (CODED) {
-        vmx = fmaxf(vmx, __shfl_xor(vmx, 16, 64));
-        vmx = fmaxf(vmx, __shfl_xor(vmx, 32, 64));
-        if (vmx > vr.limit) {
-          const float f = vr.raise(vmx);
-#pragma unroll
-          for (int n = 0; n < NQB; ++n)
-#pragma unroll
-            for (int db = 0; db < D / 16; ++db) oacc[db][n] *= f;
+          for (int db = 0; db < D / 16; ++db) oacc[db][n] *= f;
         }
       }
-    }
-    if constexpr (CODED) {
 #pragma unroll
       for (int kb = 0; kb < NK; ++kb) cvs[kb] *= vr.inv;
+      float sum[NQB];
+      f16x8 pb[BN / 32][NQB];
+      auto weigh = [&](int n) H2O_INLINE {   // returns the lane's largest
+        float x[4 * NK], top = 0.f;
+        shifted(n, mu[n], x);
+        sum[n] = 0.f;
 #pragma unroll
-      for (int kk = 0; kk < BN / 32; ++kk) {
-        f16x8 pb[NQB];
-#pragma unroll
-        for (int n = 0; n < NQB; ++n)
+        for (int kk = 0; kk < BN / 32; ++kk) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float p = __builtin_amdgcn_exp2f(x[n][8 * kk + e]);
-            l[n] += p;
-            pb[n][e] = (_Float16)(p * cvs[2 * kk + (e >> 2)][e & 3]);
+            const float p = __builtin_amdgcn_exp2f(x[8 * kk + e]);
+            sum[n] += p;
+            pb[kk][n][e] = (_Float16)(p * cvs[2 * kk + (e >> 2)][e & 3]);
           }
+          top = fmaxf(top, q8::largest(pb[kk][n]));
+        }
+        return top;
+      };
+      float top[NQB];
+      bool moves = false;
+#pragma unroll
+      for (int n = 0; n < NQB; ++n) {
+        top[n] = weigh(n);
+        moves |= top[n] >= thr[n] || sum[n] >= q8::kSum;
+      }
+      if (__builtin_amdgcn_ballot_w64(moves)) {
+#pragma unroll
+        for (int n = 0; n < NQB; ++n) {
+          float x[4 * NK], y = -INFINITY, yc = -INFINITY;
+          shifted(n, mu[n], x);
+#pragma unroll
+          for (int kb = 0; kb < NK; ++kb)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float lv = __log2f(fabsf(cvs[kb][r]));
+              y = fmaxf(y, x[4 * kb + r] + lv);
+              yc = fmaxf(yc, x[4 * kb + r] + fmaxf(lv, q8::kLeast));
+            }
+          const bool asks = q8::any_of_row(top[n] >= thr[n] || sum[n] >= q8::kSum, l16);
+          float f = 1.f;
+          if (asks) f = q8::move(mu[n], thr[n], l16, y, yc, l[n], aim);
+          l[n] *= f;
+#pragma unroll
+          for (int db = 0; db < D / 16; ++db) oacc[db][n] *= f;
+          weigh(n);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NQB; ++n) l[n] += sum[n];
+#pragma unroll
+      for (int kk = 0; kk < BN / 32; ++kk)
 #pragma unroll
         for (int db = 0; db < D / 16; ++db) {
           const f16x8 vf = __builtin_bit_cast(f16x8, tr_operand(V + 32 * kk * P, P, db, lane));
 #pragma unroll
-          for (int n = 0; n < NQB; ++n) oacc[db][n] = mma(vf, pb[n], oacc[db][n]);
+          for (int n = 0; n < NQB; ++n) oacc[db][n] = mma(vf, pb[kk][n], oacc[db][n]);
+        }
+    } else {
+      float x[NQB][4 * NK], mx[NQB];
+      bool up = false;
+#pragma unroll
+      for (int n = 0; n < NQB; ++n) {
+        shifted(n, mu[n], x[n]);
+        mx[n] = x[n][0];
+#pragma unroll
+        for (int e = 1; e < 4 * NK; ++e) mx[n] = fmaxf(mx[n], x[n][e]);
+        up |= mx[n] > thr[n];
+      }
+      if (__builtin_amdgcn_ballot_w64(up)) {
+#pragma unroll
+        for (int n = 0; n < NQB; ++n) {
+          const float y = q8::row_max(mx[n]);
+          const bool raise = y > thr[n];
+          const float f = !raise ? 1.f : thr[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(-y);
+          l[n] *= f;
+#pragma unroll
+          for (int db = 0; db < D / 16; ++db) oacc[db][n] *= f;
+          mu[n] = raise ? mu[n] + y : mu[n];
+          thr[n] = raise ? kRaise : thr[n];
+          shifted(n, mu[n], x[n]);
         }
       }
-    } else {
 #pragma unroll
       for (int kk = 0; kk < BN / 32; ++kk) {
         bf16x8 pb[NQB], rest[NQB];
@@ -407,15 +442,20 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
     };
     // turns whose tiles t + 1 and t + 2 are whole cache tiles; the other whole ones; the
     // one that ends the cache; the chunk
+    aim = q8::aim_of((t1 - t0) * BN);
     const int tm = a.M / BN, te = max(t0, min(t1, tm)), tw = max(t0, min(te, min(t1, tm) - 2));
     const int tk = max(t0, min(t1, tc));
     run(IntConst<kCache>{}, IntConst<1>{}, t0, tw);
     run(IntConst<kCache>{}, IntConst<0>{}, tw, te);
     run(IntConst<kCacheEnd>{}, IntConst<0>{}, te, tk);
+    if (Q8)
+#pragma unroll
+      for (int n = 0; n < NQB; ++n)
+        thr[n] = q8::row_max(l[n]) == 0.f ? -INFINITY : kRaise;   // cache keys seen or none
     // the chunk's values are of any size, whatever the cache's: probabilities relative to
     // a far smaller reference would leave float32
     if (Q8 && tk < t1 && vr.limit < 1.f) {
-      const float f = vr.raise(0.5f);   // to 1
+      const float f = vr.raise(0.03125f);   // to 1
 #pragma unroll
       for (int n = 0; n < NQB; ++n)
 #pragma unroll
@@ -436,7 +476,7 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
     const size_t prow = ((size_t)id.sp * BH + bh) * a.R + r;
     if (g4 == 0) {
       if (nsplit == 1) lse[orow] = (mu[n] + __log2f(L)) * kLn2;
-      else stats[prow] = make_float2(thr[n] == -INFINITY ? -INFINITY : mu[n], L);
+      else stats[prow] = make_float2(L == 0.f ? -INFINITY : mu[n], L);
     }
     const float inv = vr.ref() / L;
 #pragma unroll

@@ -1,9 +1,9 @@
 """The 8-bit cache where weights and values differ by many powers of two: what a query
 hardly attends costs what it does attend no accuracy.
 
-The values enter as codes, exactly, and their weights to 2^-16 or better; a score is off
-by 2^-16 at most here, the output is rounded by at most 2^-8 of its size: 2^-8 + 2^-11
-normwise, by query head, leaves room for the sums."""
+The values enter as codes, exactly. Their weights are rounded, each on its own, by at
+most 2^-11 of their size (small ones by 2^-11 of the largest together), the output by at
+most 2^-8 of its size: 2^-8 + 2^-11 normwise, by query head; scores are off by 2^-16 here."""
 import numpy as np
 import pytest
 import torch
@@ -78,6 +78,52 @@ SHAPES = [  # B, Hq, Hkv, d, M, T
     (1, 8, 2, 128, 2048, 1), (2, 7, 1, 64, 1501, 1), (1, 8, 2, 128, 2048, 9), (1, 4, 2, 64, 700, 40),
     (1, 16, 4, 64, 900, 150), (1, 8, 2, 128, 1100, 300),
 ]
+
+
+@pytest.mark.parametrize("where", ["first", "middle", "last"])
+@pytest.mark.parametrize("log2_size", [8, 14, 20, 60])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "-".join(map(str, s)))
+def test_a_large_value_row_of_next_to_no_weight(shape, log2_size, where):
+    """One value row 2^n times the others, at a weight of 2^-(n + 30) of theirs."""
+    B, Hq, Hkv, d, M, T = shape
+    x = inputs(*shape, "bf16", seed=log2_size)
+    at = {"first": 0, "middle": M // 2 + 5, "last": M - 1}[where]
+    s = np.zeros(M)
+    s[at] = -(log2_size + 30)
+    _weights(x, s)
+    x["v_cache"][:, :, at] *= np.float32(2.0 ** log2_size)
+    _coded(x)
+    _attend(x, f"{shape} 2^{log2_size} {where}")
+
+
+@pytest.mark.parametrize("where", [0, -1])
+@pytest.mark.parametrize("log2_weight", [16, 24, 32])
+@pytest.mark.parametrize("shape", SHAPES[:4] + [(1, 4, 1, 64, 40000, 1), (1, 4, 1, 128, 20000, 20)],
+                         ids=lambda s: "-".join(map(str, s)))
+def test_a_sink(shape, log2_weight, where):
+    """A slot that takes nearly all the weight and has no value: the output is what the
+    others add at 2^-n each."""
+    B, Hq, Hkv, d, M, T = shape
+    x = inputs(*shape, "bf16", seed=log2_weight)
+    s = np.zeros(M)
+    s[where] = log2_weight
+    _weights(x, s)
+    x["v_cache"][:, :, where] = 0.0
+    x["v_new"] *= np.float32(2.0 ** -log2_weight)
+    _coded(x)
+    _attend(x, f"{shape} sink 2^{log2_weight} at {where}")
+
+
+@pytest.mark.parametrize("d,T", [(64, 1), (128, 1), (64, 40), (128, 9), (128, 300)])
+def test_values_against_their_weights(d, T):
+    """Value rows from 2^-40 to 2^40 whose weights fall as they grow."""
+    shape = (1, 8, 2, d, 900, T)
+    x = inputs(*shape, "bf16", seed=d + T)
+    e = np.round(80 * np.arange(900) / 900 - 40)
+    _weights(x, -1.25 * e)
+    x["v_cache"] *= np.exp2(e).astype(np.float32)[:, None]
+    _coded(x)
+    _attend(x, f"against {shape}")
 
 
 @pytest.mark.parametrize("size", [2.0 ** -117, 2.0 ** -60, 2.0 ** 60, 2.0 ** 90])
