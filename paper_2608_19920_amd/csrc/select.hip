@@ -436,30 +436,35 @@ __global__ __launch_bounds__(kSelThreads) void bottomk_insert_kernel(
       keys_in, scores, token_pos, wsum, idx, M, T, k, pos0,
       [&](size_t row, const uint32_t* sidx, int i0, int i1) {
         // 16-byte vectors, four loads of each tensor in flight per thread before the stores
-        const int n = (i1 - i0) * vecs;
-        constexpr int U = 4;
-        for (int e0 = threadIdx.x; e0 < n; e0 += U * kSelThreads) {
-          uint4 kv[U], vv[U];
+        // (as uint4, a class, they were kept in memory); vecs is a power of two
+        using q8::u32x4;
+        const u32x4* ks = reinterpret_cast<const u32x4*>(kn) + row * T * vecs;
+        const u32x4* vs = reinterpret_cast<const u32x4*>(vn) + row * T * vecs;
+        u32x4* kd = reinterpret_cast<u32x4*>(kc) + row * M * vecs;
+        u32x4* vd = reinterpret_cast<u32x4*>(vc) + row * M * vecs;
+        const uint32_t n = (uint32_t)((i1 - i0) * vecs), sh = 31u - (uint32_t)__builtin_clz(vecs);
+        constexpr uint32_t U = 4;
+        for (uint32_t e0 = threadIdx.x; e0 < n; e0 += U * kSelThreads) {
+          u32x4 kv[U], vv[U];
           uint32_t slot[U];
-          int cc[U];
 #pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const int e = e0 + u * kSelThreads;
+          for (uint32_t u = 0; u < U; ++u) {
+            const uint32_t e = e0 + u * kSelThreads;
             slot[u] = 0xFFFFFFFFu;
-            cc[u] = 0;
+            kv[u] = vv[u] = u32x4{0u, 0u, 0u, 0u};
             if (e < n) {
-              const int i = i0 + e / vecs;
-              cc[u] = e % vecs;
-              kv[u] = kn[(row * T + i) * vecs + cc[u]];
-              vv[u] = vn[(row * T + i) * vecs + cc[u]];
-              slot[u] = sidx[i];
+              const size_t at = (size_t)(uint32_t)i0 * vecs + e;
+              kv[u] = ks[at];
+              vv[u] = vs[at];
+              slot[u] = sidx[i0 + (e >> sh)];
             }
           }
 #pragma unroll
-          for (int u = 0; u < U; ++u) {
+          for (uint32_t u = 0; u < U; ++u) {
             if (slot[u] < (uint32_t)M) {
-              kc[(row * M + slot[u]) * vecs + cc[u]] = kv[u];
-              vc[(row * M + slot[u]) * vecs + cc[u]] = vv[u];
+              const size_t at = (size_t)slot[u] * vecs + ((e0 + u * kSelThreads) & (vecs - 1));
+              kd[at] = kv[u];
+              vd[at] = vv[u];
             }
           }
         }
