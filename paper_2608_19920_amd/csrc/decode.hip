@@ -755,7 +755,7 @@ __device__ __forceinline__ void head_stats_load(StatIn<D>& in, const bf16_t* q, 
 template <int D>
 __device__ __forceinline__ void head_stats_from(HeadStats& hs, const StatIn<D>& in, int Hq,
                                                 int Hkv, int G, int g, int nsplit, float c_log2,
-                                                size_t bh, float* lse, bool has_chunk) {
+                                                size_t bh, float* lse, bool has_chunk, bool q8) {
   const int b = (int)(bh / Hkv), h = (int)(bh % Hkv);
   const int lane = threadIdx.x & 63;
   {
@@ -777,7 +777,9 @@ __device__ __forceinline__ void head_stats_from(HeadStats& hs, const StatIn<D>& 
     if (has_chunk) L += __builtin_amdgcn_exp2f(lnew - mx);
     if (lane < nsplit) hs.wt[lane * G + g] = wt;
     if (lane == 0) {
-      const bool any = L != 0.f;   // (a NaN, of a row of an 8-bit cache, stays one)
+      // a NaN stays one over an 8-bit cache (a row that reads back as NaN); over bf16 it counts
+      // as no weight, so that the scores of the head's other slots are not lost to it
+      const bool any = q8 ? L != 0.f : L > 0.f;
       const float lm = any ? mx + __log2f(L) : INFINITY;
       hs.lnew[g] = lnew;
       hs.lam[g] = lm;
@@ -803,12 +805,12 @@ struct StatsIn {
   }
   __device__ __forceinline__ void finish(HeadStats& hs, int Hq, int Hkv, int nsplit,
                                          float c_log2, size_t bh, float* lse,
-                                         bool has_chunk) const {
+                                         bool has_chunk, bool q8) const {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       const int g = (int)(threadIdx.x >> 6) + n * (NT / 64);
       if (g < G)
-        head_stats_from<D>(hs, in[n], Hq, Hkv, G, g, nsplit, c_log2, bh, lse, has_chunk);
+        head_stats_from<D>(hs, in[n], Hq, Hkv, G, g, nsplit, c_log2, bh, lse, has_chunk, q8);
     }
     __syncthreads();
   }
@@ -866,7 +868,7 @@ __global__ __launch_bounds__(kCombThreads) void decode_combine(
     int Hq, int Hkv, int M, int nx, int nsplit, float c_log2, const float* __restrict__ logits,
     const float2* __restrict__ dstat, const float* __restrict__ dO, bf16_t* __restrict__ out,
     float* __restrict__ lse, float* __restrict__ wsum, float* __restrict__ scores,
-    const int32_t* __restrict__ ins_idx, uint2* __restrict__ cand) {
+    const int32_t* __restrict__ ins_idx, uint2* __restrict__ cand, bool q8) {
   constexpr int NT = kCombThreads;
   __shared__ HeadStats hs;
   __shared__ uint32_t red_k[NT / 64], red_j[NT / 64];
@@ -878,7 +880,7 @@ __global__ __launch_bounds__(kCombThreads) void decode_combine(
   float* w = wsum + bh * (size_t)(M + (has_chunk ? 1 : 0));
   if ((int)blockIdx.x >= nx) {
     const int part = (int)blockIdx.x - nx, c = part * NT + tid;
-    sin.finish(hs, Hq, Hkv, nsplit, c_log2, bh, out && part == 0 ? lse : nullptr, has_chunk);
+    sin.finish(hs, Hq, Hkv, nsplit, c_log2, bh, out && part == 0 ? lse : nullptr, has_chunk, q8);
     if (out && c < G * D) {
       const int b = (int)(bh / Hkv), h = (int)(bh % Hkv);
       out[(size_t)(b * Hq + h * G) * D + c] =
@@ -904,7 +906,7 @@ __global__ __launch_bounds__(kCombThreads) void decode_combine(
     }
     if (ins_idx) ins = ins_idx[bh];
   }
-  sin.finish(hs, Hq, Hkv, nsplit, c_log2, bh, nullptr, has_chunk);
+  sin.finish(hs, Hq, Hkv, nsplit, c_log2, bh, nullptr, has_chunk, q8);
   // the lowest slot of equal keys: slots in increasing order under a strict <
   uint32_t bk = 0xFFFFFFFFu, bj = (uint32_t)c0;
   if (j0 < M) {
@@ -1055,7 +1057,7 @@ __global__ __launch_bounds__(kFinThreads) void decode_finish(
       pre[s] = has_c && s < nsplit ? dO[(bh * nsplit + s) * (size_t)(G * D) + tid] : 0.f;
     StatsIn<D, G, NT> sin;
     sin.load(q, kn, dstat, Hq, Hkv, nsplit, bh, true);
-    sin.finish(hs, Hq, Hkv, nsplit, c_log2, bh, lse, true);
+    sin.finish(hs, Hq, Hkv, nsplit, c_log2, bh, lse, true, Q8);
     if (has_c) {
       const float v = out_elem<D, kPre>(hs, vn, dO, pre, G, nsplit, bh, tid);
       const int b = (int)(bh / Hkv), h = (int)(bh % Hkv);
@@ -1093,7 +1095,7 @@ __global__ __launch_bounds__(kFinThreads) void decode_finish(
       for (int r = 0; r < kFinVec; ++r) sv[r] = sc[min(j0 + r, M - 1)];
     }
   }
-  sin.finish(hs, Hq, Hkv, nsplit, c_log2, bh, nullptr, true);
+  sin.finish(hs, Hq, Hkv, nsplit, c_log2, bh, nullptr, true, Q8);
   // A thread visits its slots in increasing order, so a strict < keeps the
   // lowest slot among equal keys. The start (max key, slot 0) is a real pair
   // whenever every key is the maximum, so the choice is always a slot of the
@@ -1275,7 +1277,8 @@ namespace {
 // lse; wsum null: nothing else. cand: leave the blocks' eviction candidates.
 hipError_t launch_combine(const Shape& s, const Plan& p, int ns, const void* q, const void* kn,
                           const void* vn, void* out, float* lse, float* wsum, float* scores,
-                          const int32_t* ins_idx, bool cand, char* ws, float c, hipStream_t st) {
+                          const int32_t* ins_idx, bool cand, char* ws, float c, hipStream_t st,
+                          bool q8 = false) {
   const int nx = wsum ? (s.M + kCombSlots - 1) / kCombSlots : 0;
   const dim3 grid(nx + (out ? (s.G() * s.d + kCombThreads - 1) / kCombThreads : 1), s.BH());
   return with_shape(s, [&](auto d, auto g) {
@@ -1284,7 +1287,7 @@ hipError_t launch_combine(const Shape& s, const Plan& p, int ns, const void* q, 
                            (const bf16_t*)kn, (const bf16_t*)vn, s.Hq, s.Hkv, s.M, nx, ns, c,
                            (const float*)(ws + p.off_logits), (const float2*)(ws + p.off_stats),
                            (const float*)(ws + p.off_opart), (bf16_t*)out, lse, wsum, scores,
-                           ins_idx, (uint2*)(ws + p.off_keys));
+                           ins_idx, (uint2*)(ws + p.off_keys), q8);
     };
     return cand ? go(decode_combine<d.value, g.value, true>)
                 : go(decode_combine<d.value, g.value, false>);
@@ -1337,7 +1340,7 @@ hipError_t launch_finish(const Shape& s, const Plan& p, bool out_too, int ns, co
   const CacheQ8 to = c8 ? *c8 : CacheQ8{};
   if (s.M > kFinSlots) {
     const hipError_t e = launch_combine(s, p, ns, q, kn, vn, out_too ? out : nullptr, lse, wsum,
-                                        scores, nullptr, true, ws, c, st);
+                                        scores, nullptr, true, ws, c, st, c8 != nullptr);
     if (e != hipSuccess) return e;
     return launch_kernel(K_DECODE_INSERT, c8 ? decode_insert<true> : decode_insert<false>,
                          dim3(s.BH()), dim3(64), st, (bf16_t*)kc, (bf16_t*)vc, to,
@@ -1433,7 +1436,8 @@ hipError_t launch_sdpa_decode_q8(const Shape& s, const Plan& p, const void* q, c
   int ns = 0;
   const hipError_t e = launch_decode_split_q8(s, p, q, c8, ws, c, st, &ns);
   if (e != hipSuccess) return e;
-  return launch_combine(s, p, ns, q, kn, vn, out, lse, wsum, nullptr, nullptr, false, ws, c, st);
+  return launch_combine(s, p, ns, q, kn, vn, out, lse, wsum, nullptr, nullptr, false, ws, c, st,
+                        true);
 }
 
 hipError_t launch_decode_step_q8(const Shape& s, const Plan& p, const void* q, const CacheQ8& c8,
