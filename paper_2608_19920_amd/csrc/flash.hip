@@ -619,7 +619,7 @@ __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void column_pass(Args a, 
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // a head's blocks, which read the same rows, on one XCD
   int bhi, bx;
-  xcd_group(blockIdx.x + gridDim.x * (blockIdx.z + gridDim.z * blockIdx.y), gridDim.x * gridDim.z,
+  xcd_group(blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z), gridDim.x * gridDim.z,
             gridDim.y, bhi, bx);
   const int bz = bx / gridDim.x;
   bx %= gridDim.x;
