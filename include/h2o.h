@@ -439,15 +439,38 @@ int h2o_sdpa_tree(const void* q, const void* k_cache, const float* k_scales,
  *   wsum[b,h,j]     = sum_{hq in group h} sum_a exp(s_{path a, j} - lse_{path a})
  *   wsum[b,h,M + c] = the same over the nodes a >= c, for the key of node path c
  *   k_acc[b,h,a,:]  = k_new[b,h,path a,:], v_acc likewise  ([B,Hkv,A,d], dtype)
- * (columns, rows and weights of entries that stand for no token are 0): wsum,
- * k_acc and v_acc are then the chunk of A tokens for h2o_accumulate_scores and
- * h2o_evict_insert, h2o_evict_insert_policy or h2o_evict_insert_q8. v_scales has
- * no part in it. */
+ * (columns, rows and weights of entries that stand for no token are 0): wsum is
+ * then what h2o_accumulate_scores adds, and wsum, k_acc and v_acc what
+ * h2o_tree_insert evicts for. Where every entry of every path is a token they are
+ * the chunk of A tokens for h2o_evict_insert, h2o_evict_insert_policy or
+ * h2o_evict_insert_q8 as well; these know nothing of a path, and would put a row of
+ * zeros, which queries attend, into a slot for every entry that is no token. v_scales
+ * has no part in it. */
 int h2o_tree_accept(const void* q, const void* k_cache, const float* k_scales,
                     const void* k_new, const void* v_new, const float* lse,
                     const int32_t* path, void* k_acc, void* v_acc, float* wsum,
                     void* workspace, size_t workspace_bytes, int B, int Hq, int Hkv,
                     int T, int M, int A, int d, float scale, int dtype, void* stream);
+
+/* Eviction and insert of the accepted nodes, whose number may differ from batch
+ * entry to batch entry: n_b entries of path[b] in [0, T) are tokens. Per (b,h): E =
+ * the n_b slots ranked lowest by `policy` as in h2o_evict_insert_policy (h2o_norm:
+ * ages against pos0[b] + n_b; h2o_orig: the first n_b of the head's shared ranking);
+ * for the token at entry a with r tokens before it, slot = E[r] in ascending order:
+ *   k_cache, v_cache[b,h,slot,:] = k_acc, v_acc[b,h,a,:] (in 8 bits with scales)
+ *   scores[b,h,slot]    = wsum[b,h,M+a]
+ *   token_pos[b,h,slot] = pos0[b] + r       (skipped when token_pos is NULL)
+ *   evict_idx[b,h,a]    = slot              (-1 for entries that are no token)
+ * All other slots are unchanged, and all of an entry without tokens. pos0 [B] int32
+ * on the device (NULL is fine without token_pos); A <= T, A <= M; workspace of
+ * h2o_evict_workspace_bytes(B, Hkv, M, A, policy). With full paths and one position
+ * the results are those of h2o_evict_insert_policy or h2o_evict_insert_q8. */
+int h2o_tree_insert(void* k_cache, float* k_scales, void* v_cache, float* v_scales,
+                    float* scores, int32_t* token_pos, const void* k_acc,
+                    const void* v_acc, const float* wsum, const int32_t* path,
+                    const int32_t* pos0, int32_t* evict_idx, int B, int Hkv, int M,
+                    int T, int A, int d, int dtype, int policy, void* workspace,
+                    size_t workspace_bytes, void* stream);
 
 /* The selection of h2o_evict_insert alone: for each of `rows` rows of M
  * float32 scores, the k smallest by (score, index), ascending indices, into

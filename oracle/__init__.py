@@ -8,11 +8,12 @@ from .h2o_oracle import (POLICIES, accumulate_scores, bottomk, decode, elem_err,
                          h2o_step, h2o_step_insert_first, kv_gather, kv_scatter, rel_err,
                          sdpa_cache, sdpa_chunk, sdpa_chunk_backward, selection_keys, visible,
                          visible_by_position)
-from .q8_tree import ancestors, dequantize, quantize, sdpa_tree, tree_accept
+from .q8_tree import ancestors, dequantize, quantize, sdpa_tree, tree_accept, tree_insert
 
 __all__ = ["POLICIES", "accumulate_scores", "bottomk", "decode", "elem_err",
            "evict_insert", "eviction_agreement",
            "h2o_step", "h2o_step_insert_first", "kv_gather", "kv_scatter", "rel_err",
            "sdpa_cache", "sdpa_chunk", "sdpa_chunk_backward", "selection_keys", "visible",
            "visible_by_position",
-           "ancestors", "dequantize", "quantize", "sdpa_tree", "tree_accept"]
+           "ancestors", "dequantize", "quantize", "sdpa_tree", "tree_accept",
+           "tree_insert"]

@@ -5,6 +5,8 @@ from typing import Optional
 
 import numpy as np
 
+from .h2o_oracle import bottomk, selection_keys
+
 F64 = np.float64
 
 
@@ -93,3 +95,31 @@ def tree_accept(q, k_cache, k_new, v_new, lse, path, scale: Optional[float] = No
                     s = scale * (K @ q[b, hq, n].astype(F64))
                     wsum[b, h, at] += np.exp(s - lse[b, hq, n])
     return wsum, k_acc, v_acc
+
+
+def tree_insert(k_cache, v_cache, scores, token_pos, k_acc, v_acc, wsum, path, pos0, T,
+                policy: str = "h2o"):
+    """Eviction and insert of a path's tokens (entries in [0, T)), whose number may differ
+    between batch entries: (k_cache, v_cache, scores, token_pos, evict_idx), new copies;
+    evict_idx is -1 at entries that are no token. pos0 [B]."""
+    path = np.asarray(path)
+    B, A = path.shape
+    Hkv, M = scores.shape[1:]
+    kc, vc, sc = k_cache.copy(), v_cache.copy(), np.asarray(scores, np.float32).copy()
+    tp = None if token_pos is None else token_pos.copy()
+    idx = np.full((B, Hkv, A), -1, np.int32)
+    for b in range(B):
+        at = [a for a in range(A) if 0 <= path[b, a] < T]
+        if not at:
+            continue
+        one = slice(None) if policy == "h2o_orig" else slice(b, b + 1)
+        keys = selection_keys(scores[one], None if token_pos is None else token_pos[one], policy,
+                              int(pos0[b]) + len(at))
+        slots = np.broadcast_to(bottomk(keys, len(at)), (1, Hkv, len(at)))[0]
+        for h in range(Hkv):
+            idx[b, h, at] = slots[h]
+            kc[b, h, slots[h]], vc[b, h, slots[h]] = k_acc[b, h, at], v_acc[b, h, at]
+            sc[b, h, slots[h]] = wsum[b, h, M + np.asarray(at)]
+            if tp is not None:
+                tp[b, h, slots[h]] = pos0[b] + np.arange(len(at), dtype=np.int32)
+    return kc, vc, sc, tp, idx

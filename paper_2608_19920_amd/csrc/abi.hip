@@ -1251,4 +1251,48 @@ int h2o_tree_accept(const void* q, const void* k_cache, const float* k_scales, c
       reinterpret_cast<hipStream_t>(stream), ScoreAcc{}));
 }
 
+int h2o_tree_insert(void* k_cache, float* k_scales, void* v_cache, float* v_scales, float* scores,
+                    int32_t* token_pos, const void* k_acc, const void* v_acc, const float* wsum,
+                    const int32_t* path, const int32_t* pos0, int32_t* evict_idx, int B, int Hkv,
+                    int M, int T, int A, int d, int dtype, int policy, void* workspace,
+                    size_t workspace_bytes, void* stream) {
+  if (T < 1) return fail(H2O_EINVAL, "tree of T = %d nodes: must be >= 1", T);
+  if (A < 1 || A > T) return fail(H2O_EINVAL, "path length A (%d) must be in [1, T = %d]", A, T);
+  if (M < A) return fail(H2O_EINVAL, "cache length M (%d) must be >= A (%d)", M, A);
+  int rc = check_rows_q8(B, Hkv, M, A, d, dtype);
+  if (!rc) rc = check_policy(policy, token_pos);
+  if (rc) return rc;
+  if (!k_cache || !v_cache || !scores || !k_acc || !v_acc || !wsum || !path || !evict_idx ||
+      (token_pos && !pos0))
+    return fail(H2O_EINVAL, "null tensor pointer");
+  if ((k_scales == nullptr) != (v_scales == nullptr))
+    return fail(H2O_EINVAL, "k_scales and v_scales go together (an 8-bit cache has both)");
+  if (!all_aligned({k_cache, k_scales, v_cache, v_scales, scores, token_pos, k_acc, v_acc, wsum,
+                    path, pos0, evict_idx, workspace}))
+    return fail(H2O_EALIGN, "tensor pointer not 16-byte aligned");
+  const size_t need = evict_workspace(B, Hkv, M, A, policy);
+  if (workspace_bytes < need || (need > 0 && !workspace))
+    return fail(H2O_EWORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, need);
+  rc = check_device();
+  if (rc) return rc;
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  const bool f32 = dtype == H2O_F32;
+  float* wk = reinterpret_cast<float*>(workspace);
+  hipError_t e = hipSuccess;
+  if (policy == H2O_POLICY_NORM)
+    e = launch_norm_keys_path(scores, token_pos, wk, path, pos0, B, Hkv, M, T, A, st);
+  if (policy == H2O_POLICY_ORIG) e = launch_orig_keys(scores, wk, B, Hkv, M, st);
+  if (e == hipSuccess)
+    e = launch_bottomk_path(policy == H2O_POLICY_H2O ? scores : wk,
+                            policy == H2O_POLICY_ORIG ? Hkv : 0, scores, token_pos, wsum, path,
+                            pos0, evict_idx, B, Hkv, M, T, A, st);
+  if (e != hipSuccess) return launched(e);
+  if (k_scales)
+    return launched(launch_kv_quantize(k_acc, v_acc, evict_idx,
+                                       CacheQ8{(int8_t*)k_cache, k_scales, (int8_t*)v_cache, v_scales},
+                                       B * Hkv, M, A, d, f32, st));
+  return launched(launch_insert(k_cache, v_cache, scores, nullptr, k_acc, v_acc, wsum, evict_idx,
+                                B * Hkv, M, A, d, A, 0, f32 ? 4 : 2, st));
+}
+
 }  // extern "C"

@@ -323,6 +323,16 @@ hipError_t launch_bottomk_insert_q8(const float* keys, float* scores, int32_t* t
                                     const CacheQ8& c, const void* kn, const void* vn,
                                     const float* wsum, int32_t* idx, int rows, int M, int T, int d,
                                     int k, int32_t pos0, bool f32, hipStream_t st);
+// The eviction after a path [B][A] (tokens: entries in [0, T)), without the rows: the
+// slots into idx [B * Hkv][A] (-1: no token), the inserted slots' scores and positions
+// (from pos0 [B]). key_rows: rows of keys shared by the batch entries, or 0.
+hipError_t launch_bottomk_path(const float* keys, int key_rows, float* scores, int32_t* token_pos,
+                               const float* wsum, const int32_t* path, const int32_t* pos0,
+                               int32_t* idx, int B, int Hkv, int M, int T, int A, hipStream_t st);
+// launch_norm_keys against t = pos0[b] and the path's tokens.
+hipError_t launch_norm_keys_path(const float* scores, const int32_t* token_pos, float* keys,
+                                 const int32_t* path, const int32_t* pos0, int B, int Hkv, int M,
+                                 int T, int A, hipStream_t st);
 hipError_t launch_kv_dequantize(const CacheQ8& c, const int32_t* idx, void* k_dst, void* v_dst,
                                 int rows, int M, int k, int d, bool f32, hipStream_t st);
 

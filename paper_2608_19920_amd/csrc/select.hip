@@ -487,6 +487,64 @@ __global__ __launch_bounds__(kSelThreads) void bottomk_insert_q8(
       });
 }
 
+// The tokens of a path: entries in [0, T) of path[b][0 .. A).
+__device__ __forceinline__ bool path_token(const int32_t* path, int i, int A, int T) {
+  return i < A && (unsigned)path[i] < (unsigned)T;
+}
+__device__ __forceinline__ int path_tokens(const int32_t* path, int A, int T) {   // whole block
+  int n = 0;
+  for (int i0 = 0; i0 < A; i0 += (int)blockDim.x)
+    n += __syncthreads_count(path_token(path, i0 + (int)threadIdx.x, A, T));
+  return n;
+}
+
+// The selection for a path, one block per row: as many slots as the path of the row's
+// batch entry has tokens; token number r of it takes the r-th of them in slot order,
+// which goes to idx[row][a] of the token's entry a (other entries: -1), its score
+// wsum[row][M + a] and position pos0[b] + r to the slot. With key_rows > 0 the keys are
+// row % key_rows of keys_in. The slots are first written side by side and then moved to
+// their entries from the last on, which are no earlier places.
+// keys_in may be the scores: a block writes its row after it has read it for good.
+// Bound by the row's selection, as bottomk_kernel (with the rows' copy after it, 8 rows of
+// 4,096 and 5 tokens 10.1 us, 32 of 32,768 and 9 tokens 20.4).
+template <bool LDS>
+__global__ __launch_bounds__(kSelThreads) void bottomk_path(
+    const float* keys_in, int key_rows, float* scores, int32_t* __restrict__ token_pos,
+    const float* __restrict__ wsum, const int32_t* __restrict__ path_all,
+    const int32_t* __restrict__ pos0, int32_t* idx_all, int Hkv, int M, int T, int A) {
+  __shared__ uint32_t keys[LDS ? kSelLdsMax + kSelLdsMax / 32 : 1];
+  __shared__ uint32_t hist[kSelBins];
+  __shared__ uint32_t tmp[2 * kSelWaves + 1];
+  __shared__ __attribute__((aligned(16))) uint32_t cand[kSelCand];
+  __shared__ uint32_t sh_ncand[2], sh_prefix, sh_krem;
+  const size_t row = blockIdx.x, b = row / Hkv;
+  const float* s = keys_in + (key_rows > 0 ? row % key_rows : row) * M;
+  const int32_t* path = path_all + b * A;
+  int32_t* idx = idx_all + row * A;
+  const int k = path_tokens(path, A, T);
+  if (k > 0) {   // uniform
+    const SelChunk c =
+        bottomk_select<LDS>(s, M, k, keys, hist, tmp, cand, sh_ncand, &sh_prefix, &sh_krem);
+    bottomk_emit<LDS>(c, s, keys, k, [&](int j, uint32_t w) { idx[w] = j; });
+  }
+  __syncthreads();
+  int left = k;
+  for (int i0 = (A - 1) / kSelThreads * kSelThreads; i0 >= 0; i0 -= kSelThreads) {
+    const int a = i0 + (int)threadIdx.x;
+    const bool on = path_token(path, a, A, T);
+    uint32_t n;
+    const int before = (int)block_exclusive_scan(on ? 1u : 0u, tmp, &n);
+    left -= (int)n;
+    const int r = left + before, slot = on ? idx[r] : -1;
+    __syncthreads();
+    if (a < A) idx[a] = slot;
+    if (on) {
+      scores[row * M + slot] = wsum[row * (size_t)(M + A) + M + a];
+      if (token_pos) token_pos[row * M + slot] = pos0[b] + r;
+    }
+  }
+}
+
 // -------------------------------------------------------------------- insert
 // Block (x, row) copies chunk keys/values i in [x*kPer, x*kPer + kPer) into
 // their evicted slots, 16 bytes per thread per step.
@@ -620,6 +678,18 @@ __global__ __launch_bounds__(256) void norm_keys_kernel(const float* __restrict_
     keys[i] = scores[i] / (float)(t - token_pos[i]);
 }
 
+// The same after a path: t = pos0[b] and the path's tokens. Block (x, b), n = Hkv * M.
+__global__ __launch_bounds__(256) void norm_keys_path_kernel(
+    const float* __restrict__ scores, const int32_t* __restrict__ token_pos,
+    float* __restrict__ keys, const int32_t* __restrict__ path, const int32_t* __restrict__ pos0,
+    size_t n, int A, int T) {
+  const size_t b = blockIdx.y;
+  const int32_t t = pos0[b] + path_tokens(path + b * A, A, T);
+  for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < n;
+       i += (size_t)gridDim.x * blockDim.x)
+    keys[b * n + i] = scores[b * n + i] / (float)(t - token_pos[b * n + i]);
+}
+
 // h2o_orig: keys[h, j] = sum over b of scores[b, h, j], float32 additions in
 // increasing b. n = Hkv * M, the size of one batch entry's scores.
 __global__ __launch_bounds__(256) void orig_keys_kernel(const float* __restrict__ scores,
@@ -658,6 +728,14 @@ hipError_t launch_norm_keys(const float* scores, const int32_t* token_pos, float
   if (n == 0) return hipSuccess;
   return launch_kernel(K_KEYS, norm_keys_kernel, dim3(flat_blocks(n)), dim3(256), st, scores,
                        token_pos, keys, n, t);
+}
+
+hipError_t launch_norm_keys_path(const float* scores, const int32_t* token_pos, float* keys,
+                                 const int32_t* path, const int32_t* pos0, int B, int Hkv, int M,
+                                 int T, int A, hipStream_t st) {
+  const size_t n = (size_t)Hkv * M;
+  return launch_kernel(K_KEYS, norm_keys_path_kernel, dim3(flat_blocks(n), B), dim3(256), st, scores,
+                       token_pos, keys, path, pos0, n, A, T);
 }
 
 hipError_t launch_orig_keys(const float* scores, float* keys, int B, int Hkv, int M,
@@ -699,6 +777,14 @@ hipError_t launch_bottomk(const float* scores, int rows, int M, int k, int32_t* 
                          scores, M, k, idx);
   return launch_kernel(K_BOTTOMK, bottomk_kernel<false>, dim3(rows), dim3(kSelThreads), st,
                        scores, M, k, idx);
+}
+
+hipError_t launch_bottomk_path(const float* keys, int key_rows, float* scores, int32_t* token_pos,
+                               const float* wsum, const int32_t* path, const int32_t* pos0,
+                               int32_t* idx, int B, int Hkv, int M, int T, int A, hipStream_t st) {
+  return launch_kernel(K_BOTTOMK, M <= kSelLdsMax ? bottomk_path<true> : bottomk_path<false>,
+                       dim3(B * Hkv), dim3(kSelThreads), st, keys, key_rows, scores, token_pos, wsum,
+                       path, pos0, idx, Hkv, M, T, A);
 }
 
 bool bottomk_insert_supported(int k) { return k >= 1 && k <= kSelBins; }

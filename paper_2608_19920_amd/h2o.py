@@ -31,6 +31,7 @@ EXPORTED = ["h2o_workspace_bytes", "h2o_sdpa_chunk", "h2o_accumulate_scores",
             "h2o_chunk_step_insert_first", "h2o_kv_quantize", "h2o_kv_dequantize",
             "h2o_q8_workspace_bytes", "h2o_sdpa_chunk_q8", "h2o_evict_insert_q8",
             "h2o_chunk_step_q8", "h2o_tree_workspace_bytes", "h2o_sdpa_tree", "h2o_tree_accept",
+            "h2o_tree_insert",
             "h2o_bottomk", "h2o_last_error", "h2o_debug_force_path",
             "h2o_debug_timing", "h2o_debug_kernel_time", "h2o_version"]
 KERNEL_IDS = {"generic_lse": 0, "generic_main": 1, "mfma_lse": 2, "mfma_main": 3,
@@ -119,6 +120,8 @@ def lib() -> ctypes.CDLL:
     L.h2o_sdpa_tree.restype = i
     L.h2o_tree_accept.argtypes = [vp] * 11 + [sz] + [i] * 7 + [f, i, vp]
     L.h2o_tree_accept.restype = i
+    L.h2o_tree_insert.argtypes = [vp] * 12 + [i] * 8 + [vp, sz, vp]
+    L.h2o_tree_insert.restype = i
     L.h2o_bottomk.argtypes = [vp, i, i, i, vp, vp]
     L.h2o_bottomk.restype = i
     L.h2o_last_error.argtypes = []
@@ -724,7 +727,8 @@ def h2o_tree_accept(q, k_cache, k_new, v_new, lse, path, k_acc, v_acc, wsum, wor
                     scale: Optional[float] = None, k_scales=None, stream=None) -> None:
     """The accepted nodes path [B,A] int32 as a chunk of A tokens: their summed
     weights wsum [B,Hkv,M+A] f32, keys and values k_acc, v_acc [B,Hkv,A,d], for
-    h2o_accumulate_scores and an h2o_evict_insert call. lse from h2o_sdpa_tree."""
+    h2o_accumulate_scores and h2o_tree_insert (or, where every entry is a token, an
+    h2o_evict_insert call). lse from h2o_sdpa_tree."""
     B, Hq, Hkv, T, M, d = _tree_args(q, k_cache, k_scales, k_new, v_new)
     if path.dtype != torch.int32 or path.dim() != 2 or path.shape[0] != B:
         raise ValueError("path must be int32 [B,A]")
@@ -744,6 +748,43 @@ def h2o_tree_accept(q, k_cache, k_new, v_new, lse, path, k_acc, v_acc, wsum, wor
                (v_acc, "v_acc"), (wsum, "wsum"), (workspace, "workspace")),
         _nbytes(workspace), B, Hq, Hkv, T, M, A, d, float(scale), _dtype_code(q),
         _stream(stream)))
+
+
+def h2o_tree_insert(k_cache, v_cache, scores, token_pos, k_acc, v_acc, wsum, path, pos0,
+                    evict_idx, T: int, policy="h2o", workspace=None, k_scales=None, v_scales=None,
+                    stream=None) -> None:
+    """Eviction and insert after h2o_tree_accept of a tree of T nodes: only the entries
+    of path [B,A] that are tokens (in [0, T)), so batch entries may have accepted
+    different numbers. pos0 [B] int32: each batch entry's next position (may be None
+    without token_pos); evict_idx [B,Hkv,A] int32, -1 for entries that are no token;
+    workspace of h2o_evict_workspace_bytes(B, Hkv, M, A, policy)."""
+    B, Hkv, M, d = k_cache.shape
+    if path.dtype != torch.int32 or path.dim() != 2 or path.shape[0] != B:
+        raise ValueError("path must be int32 [B,A]")
+    A = path.shape[1]
+    if v_cache.shape != k_cache.shape or v_cache.dtype != k_cache.dtype:
+        raise ValueError("v_cache must be like k_cache")
+    if (k_scales is None) != (v_scales is None):
+        raise ValueError("k_scales and v_scales go together")
+    if k_cache.dtype != (torch.int8 if k_scales is not None else k_acc.dtype):
+        raise TypeError("the cache must be int8 with scales, or in k_acc's dtype without")
+    for name, t in (("k_scales", k_scales), ("v_scales", v_scales)):
+        if t is not None and (t.shape != (B, Hkv, M) or t.dtype != torch.float32):
+            raise ValueError(f"{name} must be float32 [B,Hkv,M]")
+    for name, t in (("k_acc", k_acc), ("v_acc", v_acc)):
+        if t.dtype != k_acc.dtype or t.shape != (B, Hkv, A, d):
+            raise ValueError(f"{name} must be [B,Hkv,A,d] of one dtype")
+    _evict_q8(scores, token_pos, evict_idx, B, Hkv, M, A)
+    if wsum.shape != (B, Hkv, M + A) or wsum.dtype != torch.float32:
+        raise ValueError("wsum must be float32 [B,Hkv,M+A]")
+    if pos0 is not None and (pos0.dtype != torch.int32 or pos0.shape != (B,)):
+        raise ValueError("pos0 must be int32 [B]")
+    *ptrs, ws = _devs((k_cache, "k_cache"), (k_scales, "k_scales"), (v_cache, "v_cache"),
+                      (v_scales, "v_scales"), (scores, "scores"), (token_pos, "token_pos"),
+                      (k_acc, "k_acc"), (v_acc, "v_acc"), (wsum, "wsum"), (path, "path"),
+                      (pos0, "pos0"), (evict_idx, "evict_idx"), (workspace, "workspace"))
+    _check(lib().h2o_tree_insert(*ptrs, B, Hkv, M, int(T), A, d, _dtype_code(k_acc),
+                                 _policy_code(policy), ws, _nbytes(workspace), _stream(stream)))
 
 
 def h2o_bottomk(scores, k: int, idx_out, stream=None) -> None:
