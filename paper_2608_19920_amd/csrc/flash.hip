@@ -173,9 +173,10 @@ __device__ __forceinline__ void store_tile(bf16_t* Ks, bf16_t* Vs, float* sc,
 // Each of NW waves owns 16 NQB consecutive packed rows r = i*G + g. A row's
 // probabilities are exp2(x - mu) with x its scores in log2 units and mu a
 // reference common to the 4 lanes that hold the row: the maximum of the first
-// tile the row sees, raised when a score exceeds it by more than 64 (a
-// wave-uniform and rare branch), so terms stay below 2^64, far inside float32 and
-// bf16; over an 8-bit cache as q8.h says, and 15 in place of 64 in the chunk's tiles.
+// tile the row sees, raised when a score exceeds it by more than 15 (a
+// wave-uniform and rare branch), so terms stay below 2^15, and 2^20 of them times values
+// of 2^90 inside float32 (a step of 64 measured the same); over an 8-bit cache's tiles as
+// q8.h says.
 //
 // Tiles have BN keys, 32, or 64 at d = 64 with 128 rows or more, where the registers
 // allow them: half the barriers, and more of a wave's own products and exponentials to
@@ -200,7 +201,7 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
                                                          float2* __restrict__ stats,
                                                          float* __restrict__ opart) {
   constexpr int NT = NW * 64, ROWS = NW * NQB * 16, P = lds_pitch(D), NK = BN / 16;
-  constexpr float kRaise = Q8 ? 15.f : 64.f;
+  constexpr float kRaise = 15.f;
   __shared__ __attribute__((aligned(16))) bf16_t Ks[2][BN * P];
   __shared__ __attribute__((aligned(16))) bf16_t Vs[2][BN * P];
   __shared__ __attribute__((aligned(16))) float sc[2][2 * BN];
