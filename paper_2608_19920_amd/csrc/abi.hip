@@ -1260,6 +1260,7 @@ int h2o_tree_insert(void* k_cache, float* k_scales, void* v_cache, float* v_scal
   if (A < 1 || A > T) return fail(H2O_EINVAL, "path length A (%d) must be in [1, T = %d]", A, T);
   if (M < A) return fail(H2O_EINVAL, "cache length M (%d) must be >= A (%d)", M, A);
   int rc = check_rows_q8(B, Hkv, M, A, d, dtype);
+  if (!rc && (long long)B * Hkv > 65535) rc = fail(H2O_ESHAPE, "B * Hkv must be <= 65535");
   if (!rc) rc = check_policy(policy, token_pos);
   if (rc) return rc;
   if (!k_cache || !v_cache || !scores || !k_acc || !v_acc || !wsum || !path || !evict_idx ||

@@ -76,7 +76,7 @@ def _insert(L, **kw):
     (dict(policy=1, tp=None), H.H2O_EINVAL), (dict(pos0=None), H.H2O_EINVAL),
     (dict(ks=P), H.H2O_EINVAL), (dict(vs=P), H.H2O_EINVAL), (dict(policy=1), H.H2O_EWORKSPACE),
     (dict(policy=2, ws=P, wsb=16), H.H2O_EWORKSPACE), (dict(policy=2, ws=MIS, wsb=1 << 20), H.H2O_EALIGN),
-    (dict(B=1 << 20, M=512, T=256, A=256), H.H2O_ESHAPE),
+    (dict(B=1 << 20, M=512, T=256, A=256), H.H2O_ESHAPE), (dict(B=32768, Hkv=2), H.H2O_ESHAPE),
 ] + [(dict([(n, None)]), H.H2O_EINVAL) for n in ("kc", "vc", "sc", "ka", "va", "wsum", "path", "idx")]
     + [(dict([(n, MIS)]), H.H2O_EALIGN) for n in ("kc", "vc", "sc", "tp", "ka", "va", "wsum", "path",
                                                   "pos0", "idx")]
