@@ -563,7 +563,7 @@ __device__ __forceinline__ void split_q8_body(
       for (int u = 0; u < 2; ++u)
         qb[2 * x + u] = __builtin_bit_cast(bf16x8, load16(qrow + 64 * x + 8 * u));
   }
-  float m = 0.f, l = 0.f, most = -1.f;
+  float m = 0.f, l = 0.f, most = -INFINITY;
   const float aim = q8::aim_of(nst * kStep);
   q8::ValueRef ref;
   f32x4 oacc[D / 16];
@@ -597,12 +597,13 @@ __device__ __forceinline__ void split_q8_body(
       cks[kb] = *reinterpret_cast<const f32x4*>(sc + 16 * kb + 4 * grp);
       cvs[kb] = *reinterpret_cast<const f32x4*>(sc + kStep + 16 * kb + 4 * grp);
     }
-    float lg[8], vmx = 0.f;
+    float lg[8], mx = -INFINITY, vmx = 0.f;
     const bool tail = key0 + kStep > M;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       lg[i] = sacc[i >> 2][i & 3] * cks[i >> 2][i & 3];
       if (tail && key0 + 16 * (i >> 2) + 4 * grp + (i & 3) >= M) lg[i] = -INFINITY;
+      mx = fmaxf(mx, lg[i]);
       vmx = fmaxf(vmx, fabsf(cvs[i >> 2][i & 3]));
     }
 #pragma unroll
@@ -612,42 +613,33 @@ __device__ __forceinline__ void split_q8_body(
       *reinterpret_cast<f32x4*>(dst) =
           f32x4{lg[4 * kb], lg[4 * kb + 1], lg[4 * kb + 2], lg[4 * kb + 3]};
     }
-    if (__builtin_amdgcn_ballot_w64(vmx > ref.limit)) {
-      const float f = ref.raise(q8::row_max(vmx));
-      most = -1.f;
+    if (__builtin_amdgcn_ballot_w64(vmx > ref.limit ||
+                                    mx - m + q8::log2_scale(vmx * ref.inv) > most)) {
+      if (__builtin_amdgcn_ballot_w64(vmx > ref.limit)) {
+        const float f = ref.raise(q8::row_max(vmx));
+        most = -INFINITY;
 #pragma unroll
-      for (int db = 0; db < D / 16; ++db) oacc[db] *= f;
-    }
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) cvs[kb] *= ref.inv;
-    float sum;
-    f16x8 pb;
-    auto weigh = [&]() {   // (slots past M: logits -inf)
-      sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float p = __builtin_amdgcn_exp2f(lg[i] - m);
-        sum += p;
-        pb[i] = (_Float16)(p * cvs[i >> 2][i & 3]);
+        for (int db = 0; db < D / 16; ++db) oacc[db] *= f;
       }
-      return q8::largest(pb);
-    };
-    const float top = weigh();
-    if (__builtin_amdgcn_ballot_w64(top >= most || sum >= q8::kSum)) {
       float y = -INFINITY, yc = -INFINITY;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float x = lg[i] - m, lv = __log2f(fabsf(cvs[i >> 2][i & 3]));
-        y = fmaxf(y, x + lv);
-        yc = fmaxf(yc, x + fmaxf(lv, q8::kLeast));
+        const float rel = fabsf(cvs[i >> 2][i & 3]) * ref.inv;
+        y = fmaxf(y, lg[i] - m + __log2f(rel));
+        yc = fmaxf(yc, lg[i] - m + q8::log2_scale(rel));
       }
-      const bool asks = q8::any_of_row(top >= most || sum >= q8::kSum, col);
-      float f = 1.f;
-      if (asks) f = q8::move(m, most, col, y, yc, l, aim);
+      const float f = q8::move(m, most, y, yc, l, aim);
       l *= f;
 #pragma unroll
       for (int db = 0; db < D / 16; ++db) oacc[db] *= f;
-      weigh();
+    }
+    float sum = 0.f;
+    f16x8 pb;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {   // (slots past M: logits -inf)
+      const float p = __builtin_amdgcn_exp2f(lg[i] - m);
+      sum += p;
+      pb[i] = (_Float16)(p * (cvs[i >> 2][i & 3] * ref.inv));
     }
     l += sum;
 #pragma unroll

@@ -21,7 +21,7 @@
 // row's weights (q8.h), and with bf16 values split into two bf16 terms, so that next to
 // the rounding of the output theirs is small, whatever the values' and the scores' sizes
 // (1.7e-3 normwise; with probabilities in bf16 2.3e-3, and 2.8e-3 where there are few
-// rows). B1 Hq32 Hkv8 d128 M8192 T1024: 202 us; with probabilities in bf16 172, with a
+// rows). B1 Hq32 Hkv8 d128 M8192 T1024: 194 us; with probabilities in bf16 172, with a
 // reference by the scores and the largest scale, which loses rows beside a larger one that
 // nobody attends, 185, with two bf16 terms for codes as well 227.
 #include "internal.h"
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) qf[n][s] = *reinterpret_cast<const bf16x8*>(src + 32 * s);
     mu[n] = 0.f;
-    thr[n] = Q8 ? -1.f : -INFINITY;   // no tile seen yet
+    thr[n] = -INFINITY;               // no tile seen yet
     l[n] = 0.f;
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) oacc[db][n] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -301,105 +301,81 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
           x[4 * kb + r] = v;
         }
     };
-    if constexpr (CODED) {
-      float vmx = 0.f;
+    float x[NQB][4 * NK], mx[NQB], vmx = 0.f, lv = 0.f;
+    bool up = false;
+    if (CODED) {
 #pragma unroll
       for (int kb = 0; kb < NK; ++kb)
 #pragma unroll
         for (int r = 0; r < 4; ++r) vmx = fmaxf(vmx, fabsf(cvs[kb][r]));
-      if (__builtin_amdgcn_ballot_w64(vmx > vr.limit)) {
-        const float f = vr.raise(q8::row_max(vmx));
+      up = vmx > vr.limit;
+      lv = q8::log2_scale(vmx * vr.inv);
+    }
 #pragma unroll
-        for (int n = 0; n < NQB; ++n) {
-          thr[n] = -1.f;
+    for (int n = 0; n < NQB; ++n) {
+      shifted(n, mu[n], x[n]);
+      mx[n] = x[n][0];
 #pragma unroll
-          for (int db = 0; db < D / 16; ++db) oacc[db][n] *= f;
-        }
+      for (int e = 1; e < 4 * NK; ++e) mx[n] = fmaxf(mx[n], x[n][e]);
+      up |= (CODED ? mx[n] + lv : mx[n]) > thr[n];
+    }
+    if (__builtin_amdgcn_ballot_w64(up)) {
+      float fv = 1.f;
+      if (CODED && __builtin_amdgcn_ballot_w64(vmx > vr.limit)) {
+        fv = vr.raise(q8::row_max(vmx));
+#pragma unroll
+        for (int n = 0; n < NQB; ++n) thr[n] = -INFINITY;
       }
-#pragma unroll
-      for (int kb = 0; kb < NK; ++kb) cvs[kb] *= vr.inv;
-      float sum[NQB];
-      f16x8 pb[BN / 32][NQB];
-      auto weigh = [&](int n) H2O_INLINE {   // returns the lane's largest
-        float x[4 * NK], top = 0.f;
-        shifted(n, mu[n], x);
-        sum[n] = 0.f;
-#pragma unroll
-        for (int kk = 0; kk < BN / 32; ++kk) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float p = __builtin_amdgcn_exp2f(x[8 * kk + e]);
-            sum[n] += p;
-            pb[kk][n][e] = (_Float16)(p * cvs[2 * kk + (e >> 2)][e & 3]);
-          }
-          top = fmaxf(top, q8::largest(pb[kk][n]));
-        }
-        return top;
-      };
-      float top[NQB];
-      bool moves = false;
 #pragma unroll
       for (int n = 0; n < NQB; ++n) {
-        top[n] = weigh(n);
-        moves |= top[n] >= thr[n] || sum[n] >= q8::kSum;
-      }
-      if (__builtin_amdgcn_ballot_w64(moves)) {
-#pragma unroll
-        for (int n = 0; n < NQB; ++n) {
-          float x[4 * NK], y = -INFINITY, yc = -INFINITY;
-          shifted(n, mu[n], x);
+        float f;
+        if constexpr (CODED) {
+          float y = -INFINITY, yc = -INFINITY;
 #pragma unroll
           for (int kb = 0; kb < NK; ++kb)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              const float lv = __log2f(fabsf(cvs[kb][r]));
-              y = fmaxf(y, x[4 * kb + r] + lv);
-              yc = fmaxf(yc, x[4 * kb + r] + fmaxf(lv, q8::kLeast));
+              const float rel = fabsf(cvs[kb][r]) * vr.inv;
+              y = fmaxf(y, x[n][4 * kb + r] + __log2f(rel));
+              yc = fmaxf(yc, x[n][4 * kb + r] + q8::log2_scale(rel));
             }
-          const bool asks = q8::any_of_row(top[n] >= thr[n] || sum[n] >= q8::kSum, l16);
-          float f = 1.f;
-          if (asks) f = q8::move(mu[n], thr[n], l16, y, yc, l[n], aim);
-          l[n] *= f;
-#pragma unroll
-          for (int db = 0; db < D / 16; ++db) oacc[db][n] *= f;
-          weigh(n);
+          f = q8::move(mu[n], thr[n], y, yc, l[n], aim);
+        } else {
+          const float y = q8::row_max(mx[n]);
+          const bool raise = y > thr[n];
+          f = !raise ? 1.f : thr[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(-y);
+          mu[n] = raise ? mu[n] + y : mu[n];
+          thr[n] = raise ? kRaise : thr[n];
         }
+        l[n] *= f;
+        f *= fv;
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db) oacc[db][n] *= f;
+        shifted(n, mu[n], x[n]);
       }
+    }
+    if constexpr (CODED) {
 #pragma unroll
-      for (int n = 0; n < NQB; ++n) l[n] += sum[n];
+      for (int kb = 0; kb < NK; ++kb) cvs[kb] *= vr.inv;
 #pragma unroll
-      for (int kk = 0; kk < BN / 32; ++kk)
+      for (int kk = 0; kk < BN / 32; ++kk) {
+        f16x8 pb[NQB];
+#pragma unroll
+        for (int n = 0; n < NQB; ++n)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float p = __builtin_amdgcn_exp2f(x[n][8 * kk + e]);
+            l[n] += p;
+            pb[n][e] = (_Float16)(p * cvs[2 * kk + (e >> 2)][e & 3]);
+          }
 #pragma unroll
         for (int db = 0; db < D / 16; ++db) {
           const f16x8 vf = __builtin_bit_cast(f16x8, tr_operand(V + 32 * kk * P, P, db, lane));
 #pragma unroll
-          for (int n = 0; n < NQB; ++n) oacc[db][n] = mma(vf, pb[kk][n], oacc[db][n]);
+          for (int n = 0; n < NQB; ++n) oacc[db][n] = mma(vf, pb[n], oacc[db][n]);
         }
+      }
     } else {
-      float x[NQB][4 * NK], mx[NQB];
-      bool up = false;
-#pragma unroll
-      for (int n = 0; n < NQB; ++n) {
-        shifted(n, mu[n], x[n]);
-        mx[n] = x[n][0];
-#pragma unroll
-        for (int e = 1; e < 4 * NK; ++e) mx[n] = fmaxf(mx[n], x[n][e]);
-        up |= mx[n] > thr[n];
-      }
-      if (__builtin_amdgcn_ballot_w64(up)) {
-#pragma unroll
-        for (int n = 0; n < NQB; ++n) {
-          const float y = q8::row_max(mx[n]);
-          const bool raise = y > thr[n];
-          const float f = !raise ? 1.f : thr[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(-y);
-          l[n] *= f;
-#pragma unroll
-          for (int db = 0; db < D / 16; ++db) oacc[db][n] *= f;
-          mu[n] = raise ? mu[n] + y : mu[n];
-          thr[n] = raise ? kRaise : thr[n];
-          shifted(n, mu[n], x[n]);
-        }
-      }
 #pragma unroll
       for (int kk = 0; kk < BN / 32; ++kk) {
         bf16x8 pb[NQB], rest[NQB];
@@ -614,6 +590,8 @@ template <int D, bool Q8, bool PATH, int NKB, int NW>
 __global__ __launch_bounds__(NW * 64, NW == 8 ? 4 : 1) void column_pass(Args a, ColArgs p) {
   constexpr int NT = NW * 64, KB = NW * NKB * 16, P = lds_pitch(D), NU = kQRows * D / 8 / NT;
   __shared__ __attribute__((aligned(16))) bf16_t Qs[2][kQRows * P];
+  // log2(e) lse in one float32: at an lse of 20 a row's weights are off by 2^-20 together,
+  // which a sum of 64 rows and more averages (row_weight's factor in every term: 112 -> 130 us)
   __shared__ float lam[2][kQRows];
   __shared__ int pos[2][kQRows];
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
@@ -1045,8 +1023,8 @@ Args make_args(const FlashShape& s, const FlashIn& in, const char* ws, const Fla
 // and a byte of them in 1 / 3 TB/s). At B1 Hkv8 G4 T1024 d128 the plan takes 256 rows
 // and two ranges, 193 + 8 us; 128 rows 221 + 8, four ranges 206 + 13. At d64 256 rows
 // and two ranges 144 + 5, 128 rows and three 141 + 6. At T256 d128 64 rows and four
-// ranges 75 + 4 us, two 98 + 4. (All measured with the probabilities in bf16, a
-// twentieth faster in every form.)
+// ranges 75 + 4 us, two 98 + 4. (All measured with the probabilities in bf16, an
+// eighth faster in every form.)
 FlashPlan flash_plan(const FlashShape& s, bool tree) {
   FlashPlan p{};
   const long long BH = s.BH(), R = (long long)s.G() * s.T, cus = device_cus();

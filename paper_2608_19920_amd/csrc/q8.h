@@ -55,47 +55,41 @@ __device__ __forceinline__ f16x8 codes_f16(uint32_t lo, uint32_t hi) {
 // than fp16 has, in any combination (a row of large values that nobody attends, a slot
 // that takes nearly all the weight and has no value). So a row's softmax reference goes
 // by its weights: it is put where the largest of the first tile with any is 2^aim, and
-// moved there again when one reaches 2^15 (a branch of the wave, rare; the tile's weights
-// are formed again). A weight below 2^-14 is off by 2^-25, which for n keys together is
-// n 2^-(25 + aim) of the largest: 2^-11 with the aim of their number. Probabilities stay
-// below 2^90 a tile: scales are taken relative to `ref`, a power of two above all that
-// the wave has seen, and one below 2^kLeast of it counts as that much where the reference
-// is chosen. Values are lost that are 2^70 or more below the largest of their head.
-constexpr float kMost = 0x1p15f, kTop = 90.f, kSum = 0x1p90f, kLeast = -75.f;
+// moved there again when one exceeds 2^kMost. A weight below 2^-14 is off by 2^-25, which
+// for n keys together is n 2^-(25 + aim) of the largest: 2^-11 with the aim of their
+// number. Scales are taken relative to `ref`, a power of two above all that the wave has
+// seen, and one below 2^kLeast of it counts as that much where the reference is chosen,
+// so that probabilities stay below 2^90. Values are lost that are 2^70 or more below the
+// largest of their head.
+// A lane asks for more only where its largest score and its largest scale would together
+// exceed 2^kMost, as different keys' they may (a branch of the wave, rare); before the
+// exponentials, which then go out between the products. (Asked of the weights, after the
+// exponentials: B1 Hq32 Hkv8 d128 M8192 T1024 202 us.)
+constexpr float kMost = 15.f, kTop = 90.f, kLeast = -75.f;
 __device__ __forceinline__ float aim_of(int nkeys) {
   const int a = 18 - __builtin_clz(nkeys | 1);   // log2(nkeys) - 13, rounded down
   return (float)(a < 0 ? 0 : a);
 }
-// Largest of eight weights >= 0, as float32 (Inf: beyond fp16).
-__device__ __forceinline__ float largest(const f16x8& w) {
-  f16x2 m = {w[0], w[1]};
-#pragma unroll
-  for (int i = 2; i < 8; i += 2) m = __builtin_elementwise_max(m, f16x2{w[i], w[i + 1]});
-  return (float)__builtin_elementwise_max(m[0], m[1]);
-}
+// log2 of a scale relative to ref, as far as the choice of a reference counts it.
+__device__ __forceinline__ float log2_scale(float rel) { return fmaxf(__log2f(rel), kLeast); }
 __device__ __forceinline__ float row_max(float y) {   // of a row's four lanes
   y = fmaxf(y, __shfl_xor(y, 16, 64));
   return fmaxf(y, __shfl_xor(y, 32, 64));
 }
-// Whether `on` holds in one of the four lanes of this lane's row.
-__device__ __forceinline__ bool any_of_row(bool on, int l16) {
-  uint64_t b = __builtin_amdgcn_ballot_w64(on);
-  b |= b >> 32;
-  return ((uint32_t)(b | b >> 16) >> l16) & 1u;
-}
-// Moves the reference mu (log2) of the row of lane l16. y, yc: log2 of the lane's largest
-// weight of the tile, with its scale and with that no less than 2^kLeast; sofar: its sum
-// of probabilities before the tile; most: kMost, -1 before the first weight. Returns the
-// factor of the row's sums, in which probabilities stay below 2^kTop.
-__device__ __forceinline__ float move(float& mu, float& most, int l16, float y, float yc,
-                                      float sofar, float aim) {
+// Moves a row's reference mu (log2) if its largest weight asks for it. y, yc: log2 of the
+// lane's largest of the tile, with its scale and as log2_scale counts that; sofar: its
+// sum of probabilities before the tile; most: kMost, -inf before the first weight. Returns
+// the factor of the row's sums, in which probabilities stay below 2^kTop.
+__device__ __forceinline__ float move(float& mu, float& most, float y, float yc, float sofar,
+                                      float aim) {
+  y = row_max(y);
   yc = row_max(yc);
   sofar = row_max(sofar);
-  if (any_of_row(y > -INFINITY, l16)) most = kMost;
-  if (!(yc > -INFINITY)) return 1.f;
+  if (!(yc > most)) return 1.f;
   float by = yc - aim;
   if (sofar != 0.f) by = fmaxf(by, fminf(fmaxf(__log2f(sofar), -30.f) - kTop, 0.f));
   mu += by;
+  if (y > -INFINITY) most = kMost;
   return sofar == 0.f ? 1.f : __builtin_amdgcn_exp2f(-by);
 }
 // The reference of a wave's value scales, with room for 16 times what it was taken from
