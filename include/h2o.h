@@ -378,7 +378,11 @@ size_t h2o_q8_workspace_bytes(int B, int Hq, int Hkv, int T, int M, int d,
  * H2O_BF16 the products of a probability and a value's scale are rounded to fp16
  * (2^-11 of their size, small ones 2^-11 of the row's largest together), and values
  * 2^70 or more below the largest ones of their KV head may count as 0. The chunk's own
- * keys and values are in dtype. M may be 0 (the cache pointers may be NULL then). */
+ * keys and values are in dtype. M may be 0 (the cache pointers may be NULL then).
+ * In bf16, chunks of more than some 500 query rows per KV head take less time where the
+ * cache is read back once and attended in bf16 (h2o_kv_dequantize, h2o_sdpa_chunk; one
+ * layer's cache in bf16 as scratch, its values rounded): B1 Hq32 Hkv8 d128 M8192,
+ * 1,024 tokens 295 us here and 11 + 237 that way, 64 tokens 44 and 11 + 45. */
 int h2o_sdpa_chunk_q8(const void* q, const int8_t* k_codes, const float* k_scales,
                       const int8_t* v_codes, const float* v_scales,
                       const void* k_new, const void* v_new, void* out, float* lse,

@@ -114,6 +114,25 @@ def test_a_sink(shape, log2_weight, where):
     _attend(x, f"{shape} sink 2^{log2_weight} at {where}")
 
 
+@pytest.mark.slow
+@pytest.mark.parametrize("log2_weight", [18, 22, 26])
+@pytest.mark.parametrize("shape", [(1, 4, 1, 64, 60000, 1), (1, 2, 1, 128, 60000, 9), (1, 4, 1, 64, 60000, 40)],
+                         ids=lambda s: "-".join(map(str, s)))
+def test_a_sink_and_a_crowd(shape, log2_weight):
+    """A slot with nearly all the weight, and 60,000 others of 2^-n each that agree on a
+    value: small weights add up."""
+    B, Hq, Hkv, d, M, T = shape
+    x = inputs(*shape, "bf16", seed=log2_weight)
+    s = np.zeros(M)
+    s[1234] = log2_weight
+    _weights(x, s)
+    x["v_cache"][:] = 0.0
+    x["v_cache"][..., 0] = 1.0
+    x["v_cache"][:, :, 1234] = np.eye(d, dtype=np.float32)[1]
+    _coded(x)
+    _attend(x, f"{shape} crowd 2^-{log2_weight}")
+
+
 @pytest.mark.parametrize("d,T", [(64, 1), (128, 1), (64, 40), (128, 9), (128, 300)])
 def test_values_against_their_weights(d, T):
     """Value rows from 2^-40 to 2^40 whose weights fall as they grow."""
