@@ -615,12 +615,8 @@ __device__ __forceinline__ void split_q8_body(
     }
     if (__builtin_amdgcn_ballot_w64(vmx > ref.limit ||
                                     mx - m + q8::log2_scale(vmx * ref.inv) > most)) {
-      if (__builtin_amdgcn_ballot_w64(vmx > ref.limit)) {
-        const float f = ref.raise(q8::row_max(vmx));
-        most = -INFINITY;
-#pragma unroll
-        for (int db = 0; db < D / 16; ++db) oacc[db] *= f;
-      }
+      float fv = 1.f;
+      if (__builtin_amdgcn_ballot_w64(vmx > ref.limit)) fv = ref.raise(q8::row_max(vmx));
       float y = -INFINITY, yc = -INFINITY;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -628,8 +624,7 @@ __device__ __forceinline__ void split_q8_body(
         y = fmaxf(y, lg[i] - m + __log2f(rel));
         yc = fmaxf(yc, lg[i] - m + q8::log2_scale(rel));
       }
-      const float f = q8::move(m, most, y, yc, l, aim);
-      l *= f;
+      const float f = q8::move(m, most, l, fv, y, yc, aim);
 #pragma unroll
       for (int db = 0; db < D / 16; ++db) oacc[db] *= f;
     }

@@ -321,11 +321,7 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
     }
     if (__builtin_amdgcn_ballot_w64(up)) {
       float fv = 1.f;
-      if (CODED && __builtin_amdgcn_ballot_w64(vmx > vr.limit)) {
-        fv = vr.raise(q8::row_max(vmx));
-#pragma unroll
-        for (int n = 0; n < NQB; ++n) thr[n] = -INFINITY;
-      }
+      if (CODED && __builtin_amdgcn_ballot_w64(vmx > vr.limit)) fv = vr.raise(q8::row_max(vmx));
 #pragma unroll
       for (int n = 0; n < NQB; ++n) {
         float f;
@@ -339,16 +335,15 @@ __global__ __launch_bounds__(NW * 64, 2) void flash_pass(Args a, int nsplit,
               y = fmaxf(y, x[n][4 * kb + r] + __log2f(rel));
               yc = fmaxf(yc, x[n][4 * kb + r] + q8::log2_scale(rel));
             }
-          f = q8::move(mu[n], thr[n], y, yc, l[n], aim);
+          f = q8::move(mu[n], thr[n], l[n], fv, y, yc, aim);
         } else {
           const float y = q8::row_max(mx[n]);
           const bool raise = y > thr[n];
           f = !raise ? 1.f : thr[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(-y);
           mu[n] = raise ? mu[n] + y : mu[n];
           thr[n] = raise ? kRaise : thr[n];
+          l[n] *= f;
         }
-        l[n] *= f;
-        f *= fv;
 #pragma unroll
         for (int db = 0; db < D / 16; ++db) oacc[db][n] *= f;
         shifted(n, mu[n], x[n]);

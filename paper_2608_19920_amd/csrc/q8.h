@@ -76,28 +76,45 @@ __device__ __forceinline__ float row_max(float y) {   // of a row's four lanes
   y = fmaxf(y, __shfl_xor(y, 16, 64));
   return fmaxf(y, __shfl_xor(y, 32, 64));
 }
-// Moves a row's reference mu (log2) if its largest weight asks for it. y, yc: log2 of the
-// lane's largest of the tile, with its scale and as log2_scale counts that; sofar: its
-// sum of probabilities before the tile; most: kMost, -inf before the first weight. Returns
-// the factor of the row's sums, in which probabilities stay below 2^kTop.
-__device__ __forceinline__ float move(float& mu, float& most, float y, float yc, float sofar,
-                                      float aim) {
+// How far mu may go down so that a row's probabilities, sofar in a lane, stay below 2^kTop.
+__device__ __forceinline__ float least_move(float sofar) {
+  return fminf(fmaxf(__log2f(sofar), -30.f) - kTop, 0.f);
+}
+// A row's reference mu (log2) at a tile that asks for more: fv is what the scales lost by a
+// raise of theirs (or 1), and mu goes down by it, so that the weights summed so far keep
+// their size; then it moves if the tile's largest weight asks for it. y, yc: log2 of the
+// lane's largest, with its scale and as log2_scale counts that; l: its sum of probabilities;
+// most: kMost, -inf before the first weight. Returns the factor of the sums of values.
+__device__ __forceinline__ float move(float& mu, float& most, float& l, float fv, float y,
+                                      float yc, float aim) {
   y = row_max(y);
   yc = row_max(yc);
-  sofar = row_max(sofar);
-  if (!(yc > most)) return 1.f;
+  float sofar = row_max(l), fo = fv;
+  if (most > -INFINITY) {
+    const float by = fmaxf(__log2f(fv), least_move(sofar)), f = __builtin_amdgcn_exp2f(-by);
+    mu += by;
+    y -= by;
+    yc -= by;
+    l *= f;
+    sofar *= f;
+    fo *= f;
+  }
+  if (!(yc > most)) return fo;
   float by = yc - aim;
-  if (sofar != 0.f) by = fmaxf(by, fminf(fmaxf(__log2f(sofar), -30.f) - kTop, 0.f));
+  if (sofar != 0.f) by = fmaxf(by, least_move(sofar));
   mu += by;
   if (y > -INFINITY) most = kMost;
-  return sofar == 0.f ? 1.f : __builtin_amdgcn_exp2f(-by);
+  if (sofar == 0.f) return fo;
+  const float f = __builtin_amdgcn_exp2f(-by);
+  l *= f;
+  return fo * f;
 }
 // The reference of a wave's value scales, with room for 16 times what it was taken from
-// (a scale is below 2^122). After a raise the rows' references are to be moved.
+// (a scale is below 2^122).
 struct ValueRef {
   float inv = 1.f, limit = 0.f;   // 1 / ref; ref, 0 before the first keys
-  // y: the largest |scale| of the wave's keys, above limit; returns the factor of sums
-  // taken with the old reference
+  // y: the largest |scale| of the wave's keys, above limit; returns what scales and sums
+  // taken with the old reference lose
   __device__ __forceinline__ float raise(float y) {
     const uint32_t e = ((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(y)) &
                         0x7F800000u) + 5 * 0x00800000u;   // of 16 times a power of two above y

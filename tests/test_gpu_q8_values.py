@@ -96,6 +96,22 @@ def test_a_large_value_row_of_next_to_no_weight(shape, log2_size, where):
     _attend(x, f"{shape} 2^{log2_size} {where}")
 
 
+@pytest.mark.parametrize("rows", [(0, 64), (640, 704), (-64, None)])
+@pytest.mark.parametrize("log2_base,log2_size,log2_score", [(0, 60, -90), (0, 20, -120), (70, 6, -100),
+                                                            (70, 8, -300)])
+@pytest.mark.parametrize("shape", SHAPES + [(1, 2, 1, 64, 5000, 2)], ids=lambda s: "-".join(map(str, s)))
+def test_tiles_of_large_values_that_nobody_attends(shape, log2_base, log2_size, log2_score, rows):
+    """Rows of 2^base, and a run of rows 2^size larger."""
+    x = inputs(*shape, "bf16", seed=-log2_score)
+    s = np.zeros(shape[4])
+    s[slice(*rows)] = log2_score
+    _weights(x, s)
+    x["v_cache"] *= np.float32(2.0 ** log2_base)
+    x["v_cache"][:, :, slice(*rows)] *= np.float32(2.0 ** log2_size)
+    _coded(x)
+    _attend(x, f"{shape} 2^{log2_base} 2^{log2_size} at 2^{log2_score} {rows}")
+
+
 @pytest.mark.parametrize("where", [0, -1])
 @pytest.mark.parametrize("log2_weight", [16, 24, 32])
 @pytest.mark.parametrize("shape", SHAPES[:4] + [(1, 4, 1, 64, 40000, 1), (1, 4, 1, 128, 20000, 20)],
