@@ -174,3 +174,22 @@ def test_values_of_one_far_size(shape, chunk_too, size):
         x["v_new"] *= np.float32(size)
     _coded(x)
     _attend(x, f"{shape} size {size} {chunk_too}")
+
+
+@pytest.mark.parametrize("T", [1, 5, 200])
+@pytest.mark.parametrize("slots", [slice(37, 38), slice(0, 64), slice(250, 300)])
+def test_a_nan_value_row_reaches_the_output_alone(T, slots):
+    """The output of its KV head is NaN; lse, weights and the other head are as without."""
+    x = inputs(1, 4, 2, 64, 300, T, "bf16", seed=T)
+    new = [dev(x[n], BF) for n in ("q", "k_new", "v_new")]
+    runs = []
+    for nan in (False, True):
+        if nan:
+            x["v_scales"][0, 1, slots] = np.nan
+        b = H.alloc_step(1, 4, 2, T, 300, 64, BF, q8=True)
+        H.h2o_sdpa_chunk_q8(new[0], *dev_cache(x), *new[1:], b["out"], b["lse"], b["wsum"],
+                            b["workspace"], float(x["scale"]))
+        runs.append(b)
+    a, b = runs
+    assert torch.equal(a["out"][:, :2], b["out"][:, :2]) and torch.isnan(b["out"][:, 2:]).all()
+    close("bf16", "nan value", lse=(b["lse"], U.to_np(a["lse"])), wsum=(b["wsum"], U.to_np(a["wsum"])))
